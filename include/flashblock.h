@@ -353,6 +353,68 @@ fb_status fb_sparse_external_residual(const fb_shape* shape, int32_t mode, const
                                       float* m_part, float* lse_part, void* workspace,
                                       size_t workspace_bytes, void* hip_stream);
 
+/*
+ * Rotary positions.  Pair j < pairs of a head's row turns by a = p * inv_freq[j], where p is the row's position on the pair's axis:
+ *     (x, y) -> (x cos a - y sin a, x sin a + y cos a)
+ * FB_ROTARY_HALVES: x, y are elements j and j + pairs; FB_ROTARY_ADJACENT: 2 j and 2 j + 1.  Elements from 2 * pairs on stay as they are.
+ * pairs = the sum of axis_pairs[0 .. n_axes): the first axis_pairs[0] pairs take the row's position on axis 0, the next ones that on
+ * axis 1, ...  (one axis: text; three: time, height and width of a video block's tokens).  inv_freq is read as the exact number that its
+ * fp32 value is (a model's scaled frequencies are the caller's table); the angle is reduced in 64 bits, so that it is right to 1e-6 at
+ * every int32 position.  Rotation is done in fp32 and rounded once.
+ *   positions  device, int32 [batch, block_len, n_axes], batch elements position_stride elements apart (0: one list for all of
+ *              them); 4-byte aligned.  NULL (one axis only): row i of batch element b is at first[b] + offset + i.
+ *   first      device, int32 [batch], read only where positions is NULL.  NULL: zeros; in fb_append_paged the sequence's cached length.
+ */
+#define FB_MAX_ROTARY_AXES 4
+typedef enum fb_rotary_layout { FB_ROTARY_HALVES = 0, FB_ROTARY_ADJACENT = 1 } fb_rotary_layout;
+typedef struct fb_rotary {
+  uint32_t struct_size;        /* sizeof(fb_rotary), checked */
+  int32_t layout;              /* fb_rotary_layout */
+  int32_t n_axes;              /* 1 .. FB_MAX_ROTARY_AXES */
+  int32_t axis_pairs[FB_MAX_ROTARY_AXES];   /* >= 0; 1 <= sum <= head_dim / 2 */
+  int32_t offset;              /* added to first[b] + i; with listed positions it has to be 0 */
+  const float* inv_freq;       /* device [pairs] */
+  const int32_t* positions;
+  int64_t position_stride;     /* elements, >= 0 */
+  const int32_t* first;
+} fb_rotary;
+
+/* Rows of a tensor [batch, heads, block_len, head_dim] that need not be dense: row (b, h, i) starts batch_stride * b + head_stride * h +
+ * row_stride * i elements of the shape's dtype behind data (device, 16-byte aligned); its head_dim elements are contiguous.  Strides are
+ * multiples of 16 bytes and not negative; one that an index of extent 1 goes with is not looked at.  Read rows may coincide (stride 0);
+ * written rows may not (strides of at least head_dim; that rows of different indices do not overlap is the caller's to see to). */
+typedef struct fb_rows {
+  uint32_t struct_size;        /* sizeof(fb_rows), checked */
+  uint32_t reserved;           /* 0 */
+  void* data;
+  int64_t batch_stride, head_stride, row_stride;
+} fb_rows;
+
+/*
+ * A block's queries, keys and values out of the projections' layout into that of the entry points above, rotated: q -> q_out and k -> k_out
+ * by `rotary`, v -> v_out moved, in one launch.  inverse = 0: from any rows (token-major: a token's q, k and v side by side) to any
+ * rows, [B,H,Bq,d] the common case.  inverse = 1: by the opposite angles, which undoes it and, a rotation being orthogonal, is the
+ * gradient: that of q_out in q, that of q's rows out.  Each of the pairs (q, q_out), (k, k_out), (v, v_out) may be NULL, but not
+ * all three.  q has n_q_heads heads, k and v n_kv_heads; prefix_len and scale are ignored.  In place (equal data and strides) is allowed.
+ */
+fb_status fb_rotate_block(const fb_shape* shape, const fb_rotary* rotary, int32_t inverse, const fb_rows* q, const fb_rows* k,
+                          const fb_rows* v, const fb_rows* q_out, const fb_rows* k_out, const fb_rows* v_out, void* hip_stream);
+
+/*
+ * Block advance (Section 4.2: a finished block's keys and values join the prefix cache) on the paged cache, for a block, a prompt or
+ * a single token of every sequence: rows i < append_lens[b] of k and v go to slots prefix_lens[b] + i of sequence b, whose
+ * pages block_table lists; k is rotated on the way if `rotary` is given (NULL: written as it is).  The pools of kv are written;
+ * prefix_lens is read only, and lens_out [batch] (may be NULL, may not be prefix_lens) gets the new lengths.
+ *   append_lens  device, int32 [batch], clamped to [0, block_len]; NULL: block_len rows of every sequence.
+ *   q, q_out     both or neither: all block_len rows of q, rotated at the same positions, go to q_out in the same launch
+ *                (single-token decoding: what the attention after it takes).
+ * shape->prefix_len is the capacity of a sequence, at most max_pages * page_size: a row whose slot is not below it, or whose block_table
+ * entry is no page of the pool, is dropped, and lengths in lens_out end there.  Slots that no row goes to keep their contents.
+ * A page that two sequences are to write the same slot of gets one of the two.  Any page_size >= 1 is taken here.
+ */
+fb_status fb_append_paged(const fb_shape* shape, const fb_paged_kv* kv, const fb_rotary* rotary, const fb_rows* k, const fb_rows* v,
+                          const int32_t* append_lens, const fb_rows* q, const fb_rows* q_out, int32_t* lens_out, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1052,3 +1052,133 @@ fb_status fb_sparse_external_residual(const fb_shape* shape, int32_t mode, const
 }
 
 }  // extern "C"
+
+namespace {
+
+// A view's rows against the shape: FB_OK, or what is wrong with them.
+fb_status check_rows(const fb_shape* s, const fb_rows* r, int heads, bool written) {
+  if (r->struct_size != sizeof(fb_rows) || r->reserved != 0) return FB_ERR_SHAPE;
+  if (!r->data) return FB_ERR_NULL;
+  if (!aligned16(r->data)) return FB_ERR_ALIGN;
+  const int64_t esize = s->dtype == FB_BF16 ? 2 : 4;
+  const int64_t stride[3] = {r->batch_stride, r->head_stride, r->row_stride};
+  const int extent[3] = {s->batch, heads, s->block_len};
+  __int128 end = s->head_dim;
+  for (int i = 0; i < 3; ++i) {
+    if (extent[i] == 1) continue;
+    if (stride[i] < 0 || (written && stride[i] < s->head_dim)) return FB_ERR_SHAPE;
+    if (stride[i] % (16 / esize) != 0) return FB_ERR_ALIGN;
+    end += (__int128)stride[i] * (extent[i] - 1);
+  }
+  return end * esize > ((__int128)1 << 62) ? FB_ERR_SHAPE : FB_OK;
+}
+
+fb_status check_rotary(const fb_shape* s, const fb_rotary* r) {
+  if (r->struct_size != sizeof(fb_rotary)) return FB_ERR_SHAPE;
+  if (r->layout != FB_ROTARY_HALVES && r->layout != FB_ROTARY_ADJACENT) return FB_ERR_SHAPE;
+  if (r->n_axes < 1 || r->n_axes > FB_MAX_ROTARY_AXES) return FB_ERR_SHAPE;
+  long long pairs = 0;
+  for (int i = 0; i < r->n_axes; ++i) {
+    if (r->axis_pairs[i] < 0) return FB_ERR_SHAPE;
+    pairs += r->axis_pairs[i];
+  }
+  if (pairs < 1 || 2 * pairs > s->head_dim) return FB_ERR_SHAPE;
+  if (!r->inv_freq) return FB_ERR_NULL;
+  if (!aligned16(r->inv_freq) || (reinterpret_cast<uintptr_t>(r->positions) & 3u) != 0 || (reinterpret_cast<uintptr_t>(r->first) & 3u) != 0)
+    return FB_ERR_ALIGN;
+  if (r->positions) {
+    if (r->position_stride < 0 || r->position_stride > (1ll << 40) || r->offset != 0) return FB_ERR_SHAPE;
+  } else if (r->n_axes != 1) {
+    return FB_ERR_NULL;
+  }
+  return FB_OK;
+}
+
+fb::RotatePart rotate_part(const fb_rows* src, const fb_rows* dst, int heads, bool turned) {
+  fb::RotatePart p;
+  memset(&p, 0, sizeof(p));
+  if (!src) return p;
+  p.src = src->data;
+  p.s_batch = src->batch_stride; p.s_head = src->head_stride; p.s_row = src->row_stride;
+  if (dst) {
+    p.dst = dst->data;
+    p.d_batch = dst->batch_stride; p.d_head = dst->head_stride; p.d_row = dst->row_stride;
+  }
+  p.heads = heads;
+  p.turned = turned ? 1 : 0;
+  return p;
+}
+
+// Everything but the parts and the cache.
+fb::RotateParams rotate_params(const fb_shape* s, const fb_rotary* r, bool inverse) {
+  fb::RotateParams p;
+  memset(&p, 0, sizeof(p));
+  p.tokens = (uint32_t)s->batch * (uint32_t)s->block_len;
+  p.div_block = fb::make_fastdiv((uint32_t)s->block_len);
+  p.div_page = fb::make_fastdiv(1);
+  if (!r) return p;
+  p.inv_freq = r->inv_freq; p.positions = r->positions; p.first = r->first;
+  p.position_stride = r->position_stride;
+  p.adjacent = r->layout == FB_ROTARY_ADJACENT;
+  p.inverse = inverse ? 1 : 0;
+  p.n_axes = r->n_axes;
+  p.offset = r->offset;
+  for (int i = 0; i < r->n_axes; ++i) p.axis_end[i] = p.pairs += r->axis_pairs[i];
+  return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+fb_status fb_rotate_block(const fb_shape* shape, const fb_rotary* rotary, int32_t inverse, const fb_rows* q, const fb_rows* k,
+                          const fb_rows* v, const fb_rows* q_out, const fb_rows* k_out, const fb_rows* v_out, void* hip_stream) {
+  fb_status st = check_shape(shape);
+  if (st != FB_OK) return st;
+  if (!rotary) return FB_ERR_NULL;
+  if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr) || (v == nullptr) != (v_out == nullptr)) return FB_ERR_NULL;
+  if (!q && !k && !v) return FB_ERR_NULL;
+  if (inverse != 0 && inverse != 1) return FB_ERR_SHAPE;
+  if ((st = check_rotary(shape, rotary)) != FB_OK) return st;
+  const struct { const fb_rows *src, *dst; int heads; } parts[3] = {{q, q_out, shape->n_q_heads}, {k, k_out, shape->n_kv_heads}, {v, v_out, shape->n_kv_heads}};
+  fb::RotateParams p = rotate_params(shape, rotary, inverse != 0);
+  for (int i = 0; i < 3; ++i) {
+    if (parts[i].src && ((st = check_rows(shape, parts[i].src, parts[i].heads, false)) != FB_OK || (st = check_rows(shape, parts[i].dst, parts[i].heads, true)) != FB_OK)) return st;
+    p.part[i] = rotate_part(parts[i].src, parts[i].dst, parts[i].heads, i < 2);
+  }
+  hipError_t e = fb::launch_rotate(p, shape->head_dim, shape->dtype == FB_BF16, (hipStream_t)hip_stream);
+  return e == hipSuccess ? FB_OK : hip_fail(e);
+}
+
+fb_status fb_append_paged(const fb_shape* shape, const fb_paged_kv* kv, const fb_rotary* rotary, const fb_rows* k, const fb_rows* v,
+                          const int32_t* append_lens, const fb_rows* q, const fb_rows* q_out, int32_t* lens_out, void* hip_stream) {
+  fb_status st = check_shape(shape);
+  if (st != FB_OK) return st;
+  if (!kv || !k || !v || (q == nullptr) != (q_out == nullptr) || (q && !rotary)) return FB_ERR_NULL;
+  if (kv->struct_size != sizeof(fb_paged_kv)) return FB_ERR_SHAPE;
+  if (!kv->k_pool || !kv->v_pool || !kv->block_table || !kv->prefix_lens) return FB_ERR_NULL;
+  if (kv->num_pages <= 0 || kv->page_size <= 0 || kv->max_pages <= 0) return FB_ERR_SHAPE;
+  if ((long long)kv->max_pages * kv->page_size < shape->prefix_len) return FB_ERR_SHAPE;
+  if (!aligned16(kv->k_pool) || !aligned16(kv->v_pool)) return FB_ERR_ALIGN;
+  const uintptr_t out = reinterpret_cast<uintptr_t>(lens_out), lens = reinterpret_cast<uintptr_t>(kv->prefix_lens), bytes = 4 * (uintptr_t)shape->batch;
+  if (lens_out && out < lens + bytes && lens < out + bytes) return FB_ERR_UNSUPPORTED;      // other workgroups still read the lengths
+  if (((out | lens | reinterpret_cast<uintptr_t>(append_lens) | reinterpret_cast<uintptr_t>(kv->block_table)) & 3u) != 0) return FB_ERR_ALIGN;
+  if (rotary && (st = check_rotary(shape, rotary)) != FB_OK) return st;
+  if ((st = check_rows(shape, k, shape->n_kv_heads, false)) != FB_OK || (st = check_rows(shape, v, shape->n_kv_heads, false)) != FB_OK) return st;
+  if (q && ((st = check_rows(shape, q, shape->n_q_heads, false)) != FB_OK || (st = check_rows(shape, q_out, shape->n_q_heads, true)) != FB_OK)) return st;
+  fb::RotateParams p = rotate_params(shape, rotary, false);
+  p.part[0] = rotate_part(q, q_out, shape->n_q_heads, true);
+  p.part[1] = rotate_part(k, nullptr, shape->n_kv_heads, rotary != nullptr);
+  p.part[2] = rotate_part(v, nullptr, shape->n_kv_heads, false);
+  p.part[1].dst = const_cast<void*>(kv->k_pool);
+  p.part[2].dst = const_cast<void*>(kv->v_pool);
+  p.part[1].paged = p.part[2].paged = 1;
+  p.div_page = fb::make_fastdiv((uint32_t)kv->page_size);
+  p.block_table = kv->block_table; p.lens = kv->prefix_lens; p.counts = append_lens; p.lens_out = lens_out;
+  p.max_pages = kv->max_pages; p.num_pages = kv->num_pages; p.capacity = shape->prefix_len;
+  if (rotary && !rotary->positions && !rotary->first) p.first = kv->prefix_lens;
+  hipError_t e = fb::launch_rotate(p, shape->head_dim, shape->dtype == FB_BF16, (hipStream_t)hip_stream);
+  return e == hipSuccess ? FB_OK : hip_fail(e);
+}
+
+}  // extern "C"

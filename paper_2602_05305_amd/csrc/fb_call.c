@@ -18,13 +18,14 @@
 // One entry point.  Its i-th C argument (two for a W) is made of Python argument order[i] as kinds[i] says:
 //   S, K  shape, paged cache (ctypes structures): the address   P  tensor (or None): its device address
 //   W  workspace tensor (or None): address and size in bytes, two C arguments
+//   T  rotation (ctypes structure, or None): the address   R  tensor [batch, heads, rows, columns] of any strides (or None): an fb_rows
 //   I  integer                                  H  stream: None (the current one), an object with cuda_stream, or a handle
 typedef struct {
   PyObject_HEAD
   vectorcallfunc vectorcall;
   PyObject *name, *names, *defaults;         // defaults: of the last arguments
   PyObject *resolve, *stream, *check;        // name -> address; () -> current stream's handle; (status, name) raises
-  PyObject *shape, *paged;                   // types of S and K
+  PyObject *shape, *paged, *rotary;          // types of S, K and T
   PyObject *dict, *weakrefs;                 // attributes (functools.update_wrapper)
   char kinds[MAX_ARGS + 1];
   int order[MAX_ARGS];
@@ -33,9 +34,15 @@ typedef struct {
 } Call;
 
 static PyObject *g_device, *g_raw_stream;    // () -> current device, (device) -> its current stream's handle; or unset
-static PyObject *s_data_ptr, *s_numel, *s_element_size, *s_cuda_stream, *s_wrapped;
+static PyObject *s_stride, *s_data_ptr, *s_numel, *s_element_size, *s_cuda_stream, *s_wrapped;
 
 typedef int64_t A;
+typedef struct {                             // fb_rows of the library's header
+  uint32_t struct_size, reserved;
+  void* data;
+  int64_t stride[3];
+} Rows;
+#define MAX_ROWS 6
 typedef int (*F)(A, A, A, A, A, A, A, A, A, A, A, A, A, A, A, A, A, A, A, A);
 
 static int as_int(PyObject* o, A* out) {
@@ -55,14 +62,50 @@ static int from_method(PyObject* o, PyObject* method, A* out) {
   return e;
 }
 
-static int marshal(Call* c, PyObject* const* args, A* a) {
+static int as_rows(PyObject* o, Rows* out) {
+  A data;
+  if (from_method(o, s_data_ptr, &data) < 0) return -1;
+  PyObject* t = PyObject_CallMethodNoArgs(o, s_stride);
+  if (!t) return -1;
+  int e = -1;
+  A last = 0;
+  if (!PyTuple_Check(t) || PyTuple_GET_SIZE(t) != 4) {
+    PyErr_SetString(PyExc_TypeError, "a tensor [batch, heads, rows, columns] is expected");
+  } else if (as_int(PyTuple_GET_ITEM(t, 3), &last) == 0 && last != 1) {
+    PyErr_SetString(PyExc_TypeError, "the last index has to be contiguous");
+  } else {
+    e = 0;
+    for (int i = 0; i < 3 && e == 0; ++i) e = as_int(PyTuple_GET_ITEM(t, i), &out->stride[i]);
+  }
+  Py_DECREF(t);
+  out->struct_size = sizeof(Rows);
+  out->reserved = 0;
+  out->data = (void*)(intptr_t)data;
+  return e;
+}
+
+static int marshal(Call* c, PyObject* const* args, A* a, Rows* rows) {
   int n = 0;
   for (Py_ssize_t i = 0; i < c->n; ++i) {
     PyObject* o = args[c->order[i]];
     switch (c->kinds[i]) {
+      case 'R':
+        if (o == Py_None) {
+          a[n++] = 0;
+        } else {
+          if (as_rows(o, rows) < 0) return -1;
+          a[n++] = (A)(intptr_t)rows++;
+        }
+        break;
+      case 'T':
+        if (o == Py_None) {
+          a[n++] = 0;
+          break;
+        }
+        // fall through
       case 'S':
       case 'K': {
-        PyObject* type = c->kinds[i] == 'S' ? c->shape : c->paged;
+        PyObject* type = c->kinds[i] == 'S' ? c->shape : c->kinds[i] == 'K' ? c->paged : c->rotary;
         if (!PyObject_TypeCheck(o, (PyTypeObject*)type)) {
           PyErr_Format(PyExc_TypeError, "%U: %s instead of %s", c->name, Py_TYPE(o)->tp_name, ((PyTypeObject*)type)->tp_name);
           return -1;
@@ -169,7 +212,8 @@ static PyObject* call(PyObject* self, PyObject* const* args, size_t nargsf, PyOb
     c->fn = fn;
   }
   A a[MAX_ARGS] = {0};
-  if (marshal(c, bound, a) < 0) {
+  Rows rows[MAX_ROWS];
+  if (marshal(c, bound, a, rows) < 0) {
     if (!PyErr_ExceptionMatches(PyExc_TypeError) && !PyErr_ExceptionMatches(PyExc_AttributeError)) return NULL;
     return by_python(c, args, nargsf, kw);
   }
@@ -207,32 +251,36 @@ static void call_dealloc(PyObject* self) {
   Py_XDECREF(c->dict);
   Py_XDECREF(c->name); Py_XDECREF(c->names); Py_XDECREF(c->defaults);
   Py_XDECREF(c->resolve); Py_XDECREF(c->stream); Py_XDECREF(c->check); Py_XDECREF(c->shape); Py_XDECREF(c->paged);
+  Py_XDECREF(c->rotary);
   Py_TYPE(self)->tp_free(self);
 }
 
 static PyObject* call_repr(PyObject* self) { return PyUnicode_FromFormat("<native call %U>", ((Call*)self)->name); }
 
-// Call(name, names, defaults, kinds, order, resolve, stream, check, shape type, paged cache type)
+// Call(name, names, defaults, kinds, order, resolve, stream, check, shape type, paged cache type[, rotation type, for kind T])
 static PyObject* call_new(PyTypeObject* type, PyObject* args, PyObject* kw) {
-  PyObject *name, *names, *defaults, *order, *resolve, *stream, *check, *shape, *paged;
+  PyObject *name, *names, *defaults, *order, *resolve, *stream, *check, *shape, *paged, *rotary = NULL;
   const char* kinds;
   if (kw && PyDict_GET_SIZE(kw)) return PyErr_Format(PyExc_TypeError, "Call: positional arguments only");
-  if (!PyArg_ParseTuple(args, "UO!O!sO!OOOO!O!", &name, &PyTuple_Type, &names, &PyTuple_Type, &defaults, &kinds, &PyTuple_Type, &order,
-                        &resolve, &stream, &check, &PyType_Type, &shape, &PyType_Type, &paged)) return NULL;
+  if (!PyArg_ParseTuple(args, "UO!O!sO!OOOO!O!|O!", &name, &PyTuple_Type, &names, &PyTuple_Type, &defaults, &kinds, &PyTuple_Type, &order,
+                        &resolve, &stream, &check, &PyType_Type, &shape, &PyType_Type, &paged, &PyType_Type, &rotary)) return NULL;
   const Py_ssize_t n = PyTuple_GET_SIZE(names);
-  Py_ssize_t slots = 0;
+  Py_ssize_t slots = 0, views = 0;
   for (const char* k = kinds; *k; ++k) {
-    if (!strchr("SKPWIH", *k)) return PyErr_Format(PyExc_ValueError, "Call: unknown kind in '%s'", kinds);
+    if (!strchr("SKTRPWIH", *k)) return PyErr_Format(PyExc_ValueError, "Call: unknown kind in '%s'", kinds);
     slots += *k == 'W' ? 2 : 1;
+    views += *k == 'R';
+    if (*k == 'T' && !rotary) return PyErr_Format(PyExc_ValueError, "Call: '%s' without the rotation's type", kinds);
   }
-  if ((Py_ssize_t)strlen(kinds) != n || PyTuple_GET_SIZE(order) != n || slots > MAX_ARGS || PyTuple_GET_SIZE(defaults) > n)
+  if ((Py_ssize_t)strlen(kinds) != n || PyTuple_GET_SIZE(order) != n || slots > MAX_ARGS || views > MAX_ROWS || PyTuple_GET_SIZE(defaults) > n)
     return PyErr_Format(PyExc_ValueError, "Call: arguments of %U", name);
   Call* c = (Call*)type->tp_alloc(type, 0);
   if (!c) return NULL;
   c->vectorcall = call;
   Py_INCREF(name); Py_INCREF(names); Py_INCREF(defaults); Py_INCREF(resolve); Py_INCREF(stream); Py_INCREF(check); Py_INCREF(shape); Py_INCREF(paged);
+  Py_XINCREF(rotary);
   c->name = name; c->names = names; c->defaults = defaults; c->resolve = resolve; c->stream = stream; c->check = check;
-  c->shape = shape; c->paged = paged;
+  c->shape = shape; c->paged = paged; c->rotary = rotary;
   strcpy(c->kinds, kinds);
   c->n = n;
   c->fn = NULL;
@@ -284,11 +332,12 @@ static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fbcall", NULL, -1, 
 PyMODINIT_FUNC PyInit__fbcall(void) {
   if (PyType_Ready(&CallType) < 0) return NULL;
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
+  s_stride = PyUnicode_InternFromString("stride");
   s_numel = PyUnicode_InternFromString("numel");
   s_element_size = PyUnicode_InternFromString("element_size");
   s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
   s_wrapped = PyUnicode_InternFromString("__wrapped__");
-  if (!s_wrapped || !s_data_ptr || !s_numel || !s_element_size || !s_cuda_stream) return NULL;
+  if (!s_wrapped || !s_stride || !s_data_ptr || !s_numel || !s_element_size || !s_cuda_stream) return NULL;
   PyObject* m = PyModule_Create(&module);
   if (!m) return NULL;
   Py_INCREF(&CallType);

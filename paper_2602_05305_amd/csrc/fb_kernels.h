@@ -207,6 +207,27 @@ struct MaskParams {
   int B, Hq, Hkv, G, topk, nblk;
 };
 
+// Rotation of a block's rows (fb_rotary.hip).  Up to three tensors [B, heads, block_len, D] in a row, queries, keys and values; heads = 0: not
+// in this call.  Strides in elements.
+struct RotatePart {
+  const void* src; void* dst;
+  long long s_batch, s_head, s_row, d_batch, d_head, d_row;
+  int heads;
+  int turned;                 // else the rows are only moved
+  int paged;                  // dst is a pool [num_pages, heads, page_size, D]
+};
+struct RotateParams {
+  RotatePart part[3];
+  uint32_t tokens, head_groups;                // batch * block_len; workgroups along the heads
+  FastDiv div_block, div_page;
+  const float* inv_freq; const int32_t* positions; const int32_t* first;
+  long long position_stride;
+  int pairs, adjacent, inverse, n_axes, offset, axis_end[4];
+  // paged destination: row i < counts[b] (null: every row) of sequence b goes to slot lens[b] + i < capacity
+  const int32_t* block_table; const int32_t* lens; const int32_t* counts; int32_t* lens_out;
+  int max_pages, num_pages, capacity;
+};
+
 // Host-side launchers; each returns the hipError_t of its launch(es).
 hipError_t launch_attn_f32(const PassParams& p, int D, PassMode mode, hipStream_t s);
 hipError_t launch_attn_bf16(const PassParams& p, int D, PassMode mode, hipStream_t s);
@@ -231,6 +252,7 @@ hipError_t launch_block_mass_f32(const MassParams& p, int D, hipStream_t s);
 hipError_t launch_block_mass_bf16(const MassParams& p, int D, hipStream_t s);
 hipError_t launch_seq_order(const int32_t* prefix_lens, int32_t* seq_order, int B, hipStream_t s);
 hipError_t launch_head_similarity(const float* o_a, const float* o_b, float* sim, int BH, int Bq, int D, hipStream_t s);
+hipError_t launch_rotate(const RotateParams& p, int D, bool is_bf16, hipStream_t s);
 
 // Row tiles (workgroups along the group-flattened row axis) per KV group, per kernel family.
 constexpr int kRowsPerWgBf16 = 128;  // 4 waves x 32 rows

@@ -11,7 +11,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
-from ctypes import POINTER, Structure, c_char_p, c_float, c_int, c_int32, c_size_t, c_uint32, c_void_p
+from ctypes import POINTER, Structure, c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 
 try:
     from . import _fbcall                # native marshalling (csrc/fb_call.c), built with the library
@@ -25,6 +25,8 @@ FB_OK, FB_ERR_NULL, FB_ERR_SHAPE, FB_ERR_DTYPE, FB_ERR_ALIGN, FB_ERR_WORKSPACE, 
 FB_F32, FB_BF16 = 0, 1
 FB_SPARSE_REFRESH, FB_SPARSE_REUSE, FB_SPARSE_REUSE_SAME_SELECTION = 0, 1, 2
 FB_MAX_SPLITS = 256
+FB_ROTARY_HALVES, FB_ROTARY_ADJACENT = 0, 1
+FB_MAX_ROTARY_AXES = 4
 
 
 class fb_shape(Structure):
@@ -36,6 +38,16 @@ class fb_shape(Structure):
 class fb_paged_kv(Structure):
     _fields_ = [("struct_size", c_uint32), ("num_pages", c_int32), ("page_size", c_int32), ("max_pages", c_int32),
                 ("k_pool", c_void_p), ("v_pool", c_void_p), ("block_table", c_void_p), ("prefix_lens", c_void_p)]
+
+
+class fb_rotary(Structure):
+    _fields_ = [("struct_size", c_uint32), ("layout", c_int32), ("n_axes", c_int32), ("axis_pairs", c_int32 * FB_MAX_ROTARY_AXES),
+                ("offset", c_int32), ("inv_freq", c_void_p), ("positions", c_void_p), ("position_stride", c_int64), ("first", c_void_p)]
+
+
+class fb_rows(Structure):
+    _fields_ = [("struct_size", c_uint32), ("reserved", c_uint32), ("data", c_void_p), ("batch_stride", c_int64),
+                ("head_stride", c_int64), ("row_stride", c_int64)]
 
 
 class FlashBlockError(RuntimeError):
@@ -80,6 +92,9 @@ _SIGNATURES = {
                                     c_void_p, c_void_p, c_size_t, c_void_p]),
     "fb_sparse_external_residual": (c_int, [POINTER(fb_shape), c_int32, c_void_p, c_void_p, c_void_p, c_int32,
                                             c_int32] + [c_void_p] * 8 + [c_size_t, c_void_p]),
+    "fb_rotate_block": (c_int, [POINTER(fb_shape), POINTER(fb_rotary), c_int32] + [POINTER(fb_rows)] * 6 + [c_void_p]),
+    "fb_append_paged": (c_int, [POINTER(fb_shape), POINTER(fb_paged_kv), POINTER(fb_rotary), POINTER(fb_rows), POINTER(fb_rows), c_void_p,
+                                POINTER(fb_rows), POINTER(fb_rows), c_void_p, c_void_p]),
 }
 
 
@@ -319,6 +334,50 @@ def fb_sparse_external_residual(shape, mode, q, k_prefix, v_prefix, key_block, t
     _check(st, "fb_sparse_external_residual")
 
 
+def make_rotary(inv_freq, axis_pairs, layout=FB_ROTARY_HALVES, positions=None, first=None, offset=0) -> fb_rotary:
+    """inv_freq: float32 [sum(axis_pairs)]; positions: int32 [B, Bq, n_axes] or [Bq, n_axes] (one list for every batch element), contiguous but for
+    B; first: int32 [B].  The struct holds raw device addresses only: the caller keeps the tensors alive while it is in use."""
+    stride = 0
+    if positions is not None:
+        if positions.dim() not in (2, 3) or not (positions if positions.dim() == 2 else positions[0]).is_contiguous():
+            raise ValueError("positions: [Bq, n_axes] or [B, Bq, n_axes], contiguous but for B")
+        stride = positions.stride(0) if positions.dim() == 3 else 0
+    n = len(axis_pairs)
+    if not 1 <= n <= FB_MAX_ROTARY_AXES:
+        raise ValueError(f"axis_pairs: one to {FB_MAX_ROTARY_AXES} axes")
+    return fb_rotary(ctypes.sizeof(fb_rotary), layout, n, (c_int32 * FB_MAX_ROTARY_AXES)(*axis_pairs), offset, _ptr(inv_freq),
+                     _ptr(positions), stride, _ptr(first))
+
+
+def make_rows(t) -> fb_rows:
+    """t: [B, heads, Bq, d] of any strides, d contiguous."""
+    if t.dim() != 4 or t.stride(3) != 1:
+        raise ValueError("a tensor [batch, heads, rows, columns] with contiguous columns is expected")
+    return fb_rows(ctypes.sizeof(fb_rows), 0, t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+
+
+def _rows(t):
+    return None if t is None else ctypes.byref(make_rows(t))
+
+
+def _ref(s):
+    return None if s is None else ctypes.byref(s)
+
+
+def fb_rotate_block(shape, rotary, q, k, v, q_out, k_out, v_out, inverse=0, stream=None):
+    """q .. v_out: tensors [B, heads, Bq, d] of any strides, d contiguous; a pair that is not wanted is None twice."""
+    st = load_library().fb_rotate_block(_ref(shape), _ref(rotary), inverse, _rows(q), _rows(k), _rows(v), _rows(q_out), _rows(k_out),
+                                        _rows(v_out), _stream(stream))
+    _check(st, "fb_rotate_block")
+
+
+def fb_append_paged(shape, kv, rotary, k, v, append_lens=None, q=None, q_out=None, lens_out=None, stream=None):
+    """k, v, q, q_out: as in fb_rotate_block; rotary may be None."""
+    st = load_library().fb_append_paged(_ref(shape), _ref(kv), _ref(rotary), _rows(k), _rows(v), _ptr(append_lens), _rows(q), _rows(q_out),
+                                        _ptr(lens_out), _stream(stream))
+    _check(st, "fb_append_paged")
+
+
 # The entry points in native form: what each C argument is made of, in C order (fb_call.c), and where the Python order differs.  The
 # functions above stay the definition of arguments and defaults, and take what the native form does not.  (A call's marshalling 1.4 -> 0.5 us.)
 _KINDS = {
@@ -336,6 +395,11 @@ _KINDS = {
     "fb_select_topk_mass": "SPPPIIPPWH",
     "fb_sparse_external_residual": "SIPPPIIPPPPPPPWH",
 }
+# ... and those around the paged cache, which take views and a rotation
+_CACHE_KINDS = {
+    "fb_rotate_block": ("STIRRRRRRH", "shape rotary inverse q k v q_out k_out v_out stream"),
+    "fb_append_paged": "SKTRRPRRPH",
+}
 
 
 def _address(name):
@@ -343,12 +407,12 @@ def _address(name):
 
 
 def _native_calls():
-    for name, kinds in _KINDS.items():
+    for name, kinds in {**_KINDS, **_CACHE_KINDS}.items():
         fn = globals()[name]
         names = fn.__code__.co_varnames[:fn.__code__.co_argcount]
         kinds, order = kinds if isinstance(kinds, tuple) else (kinds, " ".join(names))
         call = _fbcall.Call(name, names, fn.__defaults__ or (), kinds, tuple(names.index(x) for x in order.split()),
-                            _address, lambda: _current_stream_handle(), _check, fb_shape, fb_paged_kv)
+                            _address, lambda: _current_stream_handle(), _check, fb_shape, fb_paged_kv, fb_rotary)
         globals()[name] = functools.update_wrapper(call, fn)
 
 
