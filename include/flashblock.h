@@ -415,6 +415,31 @@ fb_status fb_rotate_block(const fb_shape* shape, const fb_rotary* rotary, int32_
 fb_status fb_append_paged(const fb_shape* shape, const fb_paged_kv* kv, const fb_rotary* rotary, const fb_rows* k, const fb_rows* v,
                           const int32_t* append_lens, const fb_rows* q, const fb_rows* q_out, int32_t* lens_out, void* hip_stream);
 
+/*
+ * Attention of a batch whose sequences share a long prefix (one system prompt or document under many requests): the block-external keys of
+ * sequence b are the shared_len keys that the pages shared_pages list, the same for every sequence, and then its own
+ * prefix_lens[b] keys by block_table as in fb_external_partial_paged.  The shared keys are read once for the rows of all sequences of a
+ * KV head together, instead of once for every sequence.  Results are those of fb_external_partial_paged / fb_refresh_step_paged over the
+ * keys in a row, up to the order of floating-point sums; one call has the same bits every time.
+ *   kv            both kinds of pages are in its pools.  shape->prefix_len is the largest number of own keys; where it is 0, block_table,
+ *                 prefix_lens and max_pages are not looked at.
+ *   shared_pages  device, int32 [ceil(shared_len / page_size)], each entry clamped into the pool; NULL iff shared_len is 0.  (Shared
+ *                 keys in one dense slab [Hkv, P, d] are a pool of one page of P, a multiple of 64, keys.)
+ *   shared_len    host, >= 0, at most 2^30.  A call captured into a graph keeps it.
+ * Any of the two may be empty; with no key at all a row gets the empty partial.  workspace: >= fb_shared_workspace_bytes(shape, shared_len)
+ * bytes, 0 on invalid arguments.  (Batches above 128 sequences add the sequence-ordering launch.)
+ */
+size_t fb_shared_workspace_bytes(const fb_shape* shape, int32_t shared_len);
+fb_status fb_external_partial_shared(const fb_shape* shape, const void* q, const fb_paged_kv* kv, const int32_t* shared_pages,
+                                     int32_t shared_len, float* o_part, float* m_part, float* lse_part, void* workspace,
+                                     size_t workspace_bytes, void* hip_stream);
+/* ... and a whole refresh step: with the block-internal attention and the merge, as fb_refresh_step_paged; lse_out may be NULL.  A block of
+ * one row is single-token decoding. */
+fb_status fb_refresh_step_shared(const fb_shape* shape, const void* q, const fb_paged_kv* kv, const int32_t* shared_pages,
+                                 int32_t shared_len, const void* k_block, const void* v_block, float* o_part, float* m_part,
+                                 float* lse_part, void* out, float* lse_out, void* workspace, size_t workspace_bytes,
+                                 void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

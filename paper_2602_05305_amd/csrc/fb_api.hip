@@ -1182,3 +1182,145 @@ fb_status fb_append_paged(const fb_shape* shape, const fb_paged_kv* kv, const fb
 }
 
 }  // extern "C"
+
+namespace {
+
+// Splits of the pass over the shared keys and of the paged pass over the own ones; both store partials [split][B * Hq * Bq], the own ones
+// behind the shared ones, and what folds the splits of the other passes folds these.
+struct SharedPlan {
+  int ns_shared, ns_own;
+};
+
+// The shared keys' pass.  bf16: KV heads of more than 128 rows run 256-row workgroups, one per CU; the split count with the
+// shortest time by rounds of 256 workgroups, in tiles of 256 rows: a start and an end cost 5, a partial written and folded rows / 6700
+// (head_dim 64: half).
+int shared_splits(const fb_shape* s, int shared_len) {
+  const int tiles = (shared_len + fb::kKeyTile - 1) / fb::kKeyTile;
+  if (tiles == 0) return 0;
+  const long long nrows = rows_of(s) / s->n_kv_heads;
+  if (s->dtype != FB_BF16) {
+    const long long rt = fb::f32_row_tile(nrows), groups = s->n_kv_heads * ((nrows + rt - 1) / rt);
+    return (int)std::max(1ll, std::min({256 / groups, (long long)tiles, (long long)FB_MAX_SPLITS / 2}));
+  }
+  const bool wide = nrows > fb::kRowsPerWgBf16;
+  const long long rt = wide ? 256 : fb::kRowsPerWgBf16, groups = s->n_kv_heads * ((nrows + rt - 1) / rt);
+  const long long most = std::max(1, std::min(tiles / (wide ? 8 : 4), FB_MAX_SPLITS / 2));
+  long long best = 1, best_cost = -1;
+  for (long long ns = 1; ns <= most; ++ns) {
+    const long long cost = (groups * ns + 255) / 256 * ((tiles + ns - 1) / ns + 5) * 64 + ns * rows_of(s) * 64 / (s->head_dim == 128 ? 6700 : 13400);
+    if (best_cost < 0 || cost < best_cost) { best = ns; best_cost = cost; }
+  }
+  return (int)best;
+}
+
+SharedPlan shared_plan(const fb_shape* s, int shared_len) {
+  return {shared_splits(s, shared_len), s->prefix_len > 0 ? std::min(paged_splits(s), FB_MAX_SPLITS / 2) : 0};
+}
+
+// Everything up to the split partials; *c: what folds them.
+fb_status shared_partials(const fb_shape* shape, const void* q, const fb_paged_kv* kv, const int32_t* shared_pages, int32_t shared_len, float* o_part,
+                          float* m_part, float* lse_part, void* workspace, size_t workspace_bytes, hipStream_t stream, fb::CombineParams* c) {
+  fb_status st = check_shape(shape);
+  if (st != FB_OK) return st;
+  if (!q || !kv || !o_part || !m_part || !lse_part) return FB_ERR_NULL;
+  if (kv->struct_size != sizeof(fb_paged_kv)) return FB_ERR_SHAPE;
+  const bool own = shape->prefix_len > 0;
+  if (shared_len < 0) return FB_ERR_SHAPE;
+  if (shared_len > (1 << 30)) return FB_ERR_UNSUPPORTED;
+  if ((shared_len > 0 && !shared_pages) || (own && (!kv->block_table || !kv->prefix_lens))) return FB_ERR_NULL;
+  if ((own || shared_len > 0) && (!kv->k_pool || !kv->v_pool)) return FB_ERR_NULL;
+  if (kv->num_pages <= 0 || kv->page_size <= 0 || (own && kv->max_pages <= 0)) return FB_ERR_SHAPE;
+  if (kv->page_size % fb::kKeyTile != 0) return FB_ERR_UNSUPPORTED;
+  if (own && (long long)kv->max_pages * kv->page_size < shape->prefix_len) return FB_ERR_SHAPE;
+  if (!aligned16(q) || !aligned16(kv->k_pool) || !aligned16(kv->v_pool) || !aligned16(o_part) || !aligned16(m_part) || !aligned16(lse_part) || !aligned16(workspace))
+    return FB_ERR_ALIGN;
+  if (((reinterpret_cast<uintptr_t>(shared_pages) | reinterpret_cast<uintptr_t>(kv->block_table) | reinterpret_cast<uintptr_t>(kv->prefix_lens)) & 3u) != 0) return FB_ERR_ALIGN;
+  const long long G = shape->n_q_heads / shape->n_kv_heads, group = G * shape->block_len, gap = (long long)(shape->n_q_heads - G) * shape->block_len;
+  // (bf16: the 256 query rows of a workgroup are addressed within 32 bits of each other)
+  if (shape->dtype == FB_BF16 && (std::min(255 / group + 1, shape->batch - 1ll) * gap + 256) * shape->head_dim * 2 >= (1ll << 32)) return FB_ERR_UNSUPPORTED;
+  const SharedPlan plan = shared_plan(shape, shared_len);
+  const int ns = plan.ns_shared + plan.ns_own;
+  const WsLayout w = ws_layout(shape, ns, 1, 0);
+  if (!workspace || workspace_bytes < w.total) return FB_ERR_WORKSPACE;
+
+  char* ws = (char*)workspace;
+  const size_t rows = (size_t)rows_of(shape), behind = plan.ns_shared * rows;
+  float *ws_o = (float*)(ws + w.o[0]), *ws_m = (float*)(ws + w.m[0]), *ws_l = (float*)(ws + w.l[0]);
+  if (plan.ns_shared > 0) {
+    fb::PassParams p = base_pass(shape, q, kv->k_pool, kv->v_pool, shared_len, plan.ns_shared);
+    p.ws_o = ws_o; p.ws_m = ws_m; p.ws_l = ws_l;
+    p.B = 1;
+    p.Bq = shape->batch * shape->block_len;
+    p.key_block = (int)group;
+    p.nblk = (int)gap;
+    p.block_table = shared_pages; p.page_size = kv->page_size; p.num_pages = kv->num_pages;
+    const hipError_t e = launch_attn(shape, p, fb::kPassShared, stream);
+    if (e != hipSuccess) return hip_fail(e);
+  }
+  if (plan.ns_own > 0) {
+    fb::PassParams p = base_pass(shape, q, kv->k_pool, kv->v_pool, shape->prefix_len, plan.ns_own);
+    p.ws_o = ws_o + behind * shape->head_dim; p.ws_m = ws_m + behind; p.ws_l = ws_l + behind;
+    p.block_table = kv->block_table; p.prefix_lens = kv->prefix_lens;
+    p.page_size = kv->page_size; p.max_pages = kv->max_pages; p.num_pages = kv->num_pages;
+    if (shape->batch > 1 && shape->batch <= 128 && shape->dtype == FB_BF16) {
+      p.order_inline = 1;
+    } else if (shape->batch > 1) {
+      p.seq_order = (int32_t*)(ws + w.order);
+      const hipError_t e = fb::launch_seq_order(kv->prefix_lens, (int32_t*)(ws + w.order), shape->batch, stream);
+      if (e != hipSuccess) return hip_fail(e);
+    }
+    const hipError_t e = launch_attn(shape, p, fb::kPassDensePaged, stream);
+    if (e != hipSuccess) return hip_fail(e);
+  }
+  memset(c, 0, sizeof(*c));
+  c->rows = (int)rows; c->D = shape->head_dim; c->nsplit = ns;
+  c->ws_o = ws_o; c->ws_m = ws_m; c->ws_l = ws_l;
+  c->o = o_part; c->m = m_part; c->lse = lse_part;
+  c->Bq = shape->block_len;
+  c->Hq = shape->n_q_heads; c->Hkv = shape->n_kv_heads; c->G = (int)G;
+  return FB_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t fb_shared_workspace_bytes(const fb_shape* shape, int32_t shared_len) {
+  if (check_shape(shape) != FB_OK || shared_len < 0 || shared_len > (1 << 30)) return 0;
+  const SharedPlan plan = shared_plan(shape, shared_len);
+  return std::max((size_t)256, ws_layout(shape, plan.ns_shared + plan.ns_own, 1, 0).total);
+}
+
+fb_status fb_external_partial_shared(const fb_shape* shape, const void* q, const fb_paged_kv* kv, const int32_t* shared_pages,
+                                     int32_t shared_len, float* o_part, float* m_part, float* lse_part, void* workspace,
+                                     size_t workspace_bytes, void* hip_stream) {
+  fb::CombineParams c;
+  const fb_status st = shared_partials(shape, q, kv, shared_pages, shared_len, o_part, m_part, lse_part, workspace, workspace_bytes,
+                                       (hipStream_t)hip_stream, &c);
+  if (st != FB_OK) return st;
+  const hipError_t e = fb::launch_combine(c, (hipStream_t)hip_stream);
+  return e == hipSuccess ? FB_OK : hip_fail(e);
+}
+
+fb_status fb_refresh_step_shared(const fb_shape* shape, const void* q, const fb_paged_kv* kv, const int32_t* shared_pages,
+                                 int32_t shared_len, const void* k_block, const void* v_block, float* o_part, float* m_part,
+                                 float* lse_part, void* out, float* lse_out, void* workspace, size_t workspace_bytes,
+                                 void* hip_stream) {
+  fb_status st = check_shape(shape);
+  if (st != FB_OK) return st;
+  if (!k_block || !v_block || !out) return FB_ERR_NULL;
+  if (!aligned16(k_block) || !aligned16(v_block) || !aligned16(out) || !aligned16(lse_out)) return FB_ERR_ALIGN;
+  fb::CombineParams c;
+  hipStream_t stream = (hipStream_t)hip_stream;
+  st = shared_partials(shape, q, kv, shared_pages, shared_len, o_part, m_part, lse_part, workspace, workspace_bytes, stream, &c);
+  if (st != FB_OK) return st;
+  hipError_t e = fb::launch_combine(c, stream);
+  if (e != hipSuccess) return hip_fail(e);
+  fb::PassParams in = base_pass(shape, q, k_block, v_block, shape->block_len, 1);
+  in.out = out; in.lse_out = lse_out;
+  in.ext_o = o_part; in.ext_m = m_part; in.ext_lse = lse_part;
+  e = launch_attn(shape, in, fb::kPassInternal, stream);
+  return e == hipSuccess ? FB_OK : hip_fail(e);
+}
+
+}  // extern "C"

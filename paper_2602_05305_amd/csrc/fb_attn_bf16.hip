@@ -1268,6 +1268,7 @@ hipError_t launch_d(const PassParams& p, PassMode mode, hipStream_t s) {
       if (p.nsplit > 1) return launch_one<D, kPassSparseReuse, kKeyTile, 1, 2>(p, s);
       return launch_one<D, kPassSparseReuse, kKeyTile, 1, 1>(p, s);
     case kPassRefreshOne: break;                 // fp32 only
+    case kPassShared: break;                     // the streaming kernel's
   }
   return hipErrorInvalidValue;
 }

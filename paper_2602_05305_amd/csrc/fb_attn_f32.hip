@@ -354,7 +354,8 @@ __device__ __forceinline__ bool f32_pass(const PassParams& p, unsigned char* rin
   if constexpr (MODE == kPassDensePaged) nkeys = min(p.nkeys, max(0, sload(p.prefix_lens, b)));   // this sequence's prefix
 
   // contiguous cache: this KV head's [nkeys, D] slab; paged cache: the pool (tiles add their page offset)
-  const size_t slab = (MODE == kPassDensePaged) ? (size_t)0 : (size_t)bk * nkeys * C::ROWB;
+  constexpr bool kPages = MODE == kPassDensePaged || MODE == kPassShared;
+  const size_t slab = kPages ? (size_t)0 : (size_t)bk * nkeys * C::ROWB;
   const unsigned char* __restrict__ Kg = (const unsigned char*)(own_block ? p.k2 : p.k) + slab;
   const unsigned char* __restrict__ Vg = (const unsigned char*)(own_block ? p.v2 : p.v) + slab;
 
@@ -395,7 +396,7 @@ __device__ __forceinline__ bool f32_pass(const PassParams& p, unsigned char* rin
           t.is_sel = ((mask >> (unit_h - kvh * p.G)) & 1u) != 0u;
         }
       }
-      if constexpr (MODE == kPassDensePaged) {
+      if constexpr (kPages) {                                   // (kPassShared: b is 0)
         const int slot = (int)fastdiv((uint32_t)t.k0, p.div_page);
         const int page = min(max(sload(p.block_table + (size_t)b * p.max_pages, slot), 0), p.num_pages - 1);
         t.off = (((size_t)page * p.Hkv + kvh) * p.page_size + (t.k0 - slot * (int)p.div_page.d)) * C::ROWB;
@@ -445,7 +446,7 @@ __device__ __forceinline__ bool f32_pass(const PassParams& p, unsigned char* rin
   f32x4 q[RB][C::NQ];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    const float* qr = (const float*)p.q + (grow_base + min(row0 + 16 * rb + l16, nrows - 1)) * D + 4 * g4;
+    const float* qr = (const float*)p.q + (MODE == kPassShared ? shared_row(p, kvh, min(row0 + 16 * rb + l16, nrows - 1)) : grow_base + min(row0 + 16 * rb + l16, nrows - 1)) * D + 4 * g4;
 #pragma unroll
     for (int j = 0; j < C::NQ; ++j) q[rb][j] = *(const f32x4*)(qr + 16 * j);
   }
@@ -660,7 +661,7 @@ __device__ __forceinline__ bool f32_pass(const PassParams& p, unsigned char* rin
         } else {
           const bool set1 = own_block || i == 1;              // residual keys, or the block's own keys
           const size_t rows_total = (size_t)p.B * p.Hq * p.Bq;
-          const size_t wrow = (own_block ? (size_t)0 : (size_t)split * rows_total) + grow;
+          const size_t wrow = (own_block ? (size_t)0 : (size_t)split * rows_total) + (MODE == kPassShared ? shared_row(p, kvh, row) : grow);
           float* __restrict__ w_o = set1 ? p.ws_o2 : p.ws_o;
           float* __restrict__ w_m = set1 ? p.ws_m2 : p.ws_m;
           float* __restrict__ w_l = set1 ? p.ws_l2 : p.ws_l;
@@ -1008,7 +1009,8 @@ hipError_t launch_f32(const PassParams& p, hipStream_t s) {
   if (MODE == kPassDensePaged) units = (units + 7) / 8 * 8;
   if (units * rowtiles >= (1ll << 31)) return hipErrorInvalidValue;
   PassParams q = p;
-  if (MODE == kPassDensePaged) q.div_page = make_fastdiv((uint32_t)p.page_size);
+  if (MODE == kPassDensePaged || MODE == kPassShared) q.div_page = make_fastdiv((uint32_t)p.page_size);
+  if (MODE == kPassShared) q.div_tpb = make_fastdiv((uint32_t)p.key_block);
   q.div_rowtiles = make_fastdiv((uint32_t)rowtiles);
   q.div_nsplit = make_fastdiv((uint32_t)nsplit);
   q.div_hkv = make_fastdiv((uint32_t)heads);
@@ -1071,6 +1073,7 @@ hipError_t launch_d(const PassParams& p, PassMode mode, hipStream_t s) {
     case kPassDenseHeads: return launch_f32_rows<D, kPassDenseHeads>(p, s);
     case kPassDensePaged: return launch_f32_rows<D, kPassDensePaged>(p, s);
     case kPassRefreshFused: return launch_f32_rows<D, kPassRefreshFused>(p, s);
+    case kPassShared: return launch_f32_rows<D, kPassShared>(p, s);
     case kPassRefreshOne: return launch_f32<D, kPassRefreshOne, 1, 1, D == 64 ? 2 : 1>(p, s);      // (the caller has checked f32_refresh_one)
   }
   return hipErrorInvalidValue;

@@ -92,7 +92,8 @@ enum PassMode : int {
   kPassDensePaged = 5,     // dense over a paged KV pool with a block table and per-sequence prefix lengths
   kPassRefreshFused = 6,   // dense over the prefix, and the block's own keys into partial set 1: in the last split's workgroup
                            // (register-staged), as an extra split (fp32), as two streams or not at all (by_parity)
-  kPassRefreshOne = 7      // fp32: a whole refresh step in one kernel (prefix unsplit, final partial, then the block and the merge)
+  kPassRefreshOne = 7,     // fp32: a whole refresh step in one kernel (prefix unsplit, final partial, then the block and the merge)
+  kPassShared = 8          // dense over one list of pages (block_table, nkeys keys), for the rows of a KV head in all sequences together
 };
 
 // One attention pass.  Rows of one KV group are addressed "group-flattened": query head
@@ -111,7 +112,8 @@ struct PassParams {
   // internal pass epilogue
   const float* ext_o; const float* ext_m; const float* ext_lse;   // cached partial (natural log), may be null
   void* out; float* lse_out;
-  // sparse passes
+  // sparse passes.  (kPassShared: B is 1 and Bq the sequences' rows of a query head together, so that a KV head's rows are those of sequence
+  // 0, sequence 1, ..., key_block = G * block_len to each, with nblk rows of other KV heads between them in q and in the partials)
   const uint32_t* blk_mask;   // [B,Hkv,nblk] bit g set: head g of the group selected the block
   const int32_t* union_list;  // [B,Hkv,nblk] ascending blocks with mask != 0
   const uint32_t* union_mask; // [B,Hkv,nblk] mask of the i-th listed block (no dependent lookup in the reuse pass)
@@ -155,7 +157,7 @@ struct PassParams {
   FastDiv div_page;                            // bf16 paged pass: key index -> page slot
   FastDiv div_bias;                            // streaming bf16 pass, xcd_bias: by 64 * nsplit
   FastDiv div_tpb;                             // streaming sparse passes: tile index -> key block (tiles per key block); per-head
-                                               // refresh by rank: row -> head (block_len)
+                                               // refresh by rank: row -> head (block_len); kPassShared: row -> sequence (key_block)
 };
 
 // Fold split partials (and optionally a cached residual) into final (o, m, lse) partials.
@@ -312,6 +314,15 @@ inline bool dense_row_pairs(int nrows, int head_dim) {
 inline bool internal_many_rows(const PassParams& p) {
   const int nrows = p.G * p.Bq;
   return nrows >= 1024 && (long long)p.B * p.Hkv * ((nrows + 255) / 256) >= 128;
+}
+
+// Rows of q between the first row of a workgroup, row0 of its KV head, and the row r of the head (kPassShared).
+__device__ __forceinline__ int shared_row_offset(const PassParams& p, int row0, int r) {
+  return r - row0 + ((int)fastdiv((uint32_t)r, p.div_tpb) - (int)fastdiv((uint32_t)row0, p.div_tpb)) * p.nblk;
+}
+// Row of q that row0 of KV head kvh is.
+__device__ __forceinline__ size_t shared_row(const PassParams& p, int kvh, int row0) {
+  return (size_t)kvh * p.key_block + row0 + (size_t)fastdiv((uint32_t)row0, p.div_tpb) * p.nblk;
 }
 
 // ---- device helpers shared by the attention kernels -------------------------------------

@@ -218,8 +218,9 @@ __device__ __forceinline__ void rows_pass(const PassParams& p, unsigned char* ri
     return r + (__shfl(head_of, k, 64) - k) * p.Bq;
   };
 
-  const unsigned char* __restrict__ Kg = (const unsigned char*)(own_block ? p.k2 : p.k) + (size_t)bk * nkeys * C::ROWB;
-  const unsigned char* __restrict__ Vg = (const unsigned char*)(own_block ? p.v2 : p.v) + (size_t)bk * nkeys * C::ROWB;
+  constexpr bool kShared = MODE == kPassShared;              // keys in pages of a pool
+  const unsigned char* __restrict__ Kg = (const unsigned char*)(own_block ? p.k2 : p.k) + (kShared ? (size_t)0 : (size_t)bk * nkeys * C::ROWB);
+  const unsigned char* __restrict__ Vg = (const unsigned char*)(own_block ? p.v2 : p.v) + (kShared ? (size_t)0 : (size_t)bk * nkeys * C::ROWB);
 
   // ---- tiles of this workgroup: positions first, first + stride, ... of a range, rotated (per-head refresh, partials by rank, and refresh
   // step: splits 2i and 2i + 1 take the even and the odd tiles of the i-th range, the two tile groups of the register-staged kernel,
@@ -296,8 +297,37 @@ __device__ __forceinline__ void rows_pass(const PassParams& p, unsigned char* ri
     return st;
   };
   Stream kst = open_stream(Kg), vst = open_stream(Vg);
+  // kShared: the page of the tile that K's next step asks for, looked up a step ahead; V's steps come one behind K's and take its offset
+  int32_t page = 0;
+  int slot = 0, in_page = 0;                                 // tiles
+  size_t off_now = 0, off_before = 0;
+  const int page_tiles = kShared ? p.page_size / C::KT : 1;
+  if constexpr (kShared) {
+    const int tile = tr.begin + kst.at;
+    slot = (int)fastdiv((uint32_t)(tile * C::KT), p.div_page);
+    in_page = tile - slot * page_tiles;
+    page = sload(p.block_table, slot);
+  }
+  auto step_pages = [&]() __attribute__((always_inline)) {
+    off_before = off_now;
+    off_now = ((size_t)min(max(page, 0), p.num_pages - 1) * p.Hkv + kvh) * ((size_t)p.page_size * C::ROWB) + (size_t)in_page * C::OPB;
+    kst.src = Kg + off_now;
+    const bool wrap = ++kst.at == range, turn = ++in_page == page_tiles;
+    if (wrap) {
+      kst.at = 0;
+      slot = (int)fastdiv((uint32_t)(tr.begin * C::KT), p.div_page);
+      in_page = tr.begin - slot * page_tiles;
+    } else if (turn) {
+      in_page = 0;
+      ++slot;
+    }
+    page = sload(p.block_table, slot);
+  };
   auto step_stream = [&](Stream& st) __attribute__((always_inline)) {
-    if constexpr (kParity) {
+    if constexpr (kShared) {
+      if (&st == &kst) step_pages();
+      else st.src = Vg + off_before;
+    } else if constexpr (kParity) {
       st.src = st.left > 0 ? st.next : st.first;
       --st.left;
       st.at += stride;
@@ -325,7 +355,7 @@ __device__ __forceinline__ void rows_pass(const PassParams& p, unsigned char* ri
   // prologue
   {
     const int at = kHeads ? __builtin_amdgcn_readfirstlane(group_row(row0)) : row0;
-    const unsigned char* qg = (const unsigned char*)p.q + (grow_base + at) * C::ROWB;
+    const unsigned char* qg = (const unsigned char*)p.q + (kShared ? shared_row(p, kvh, row0) : grow_base + at) * C::ROWB;
     const int qvalid = nflagged - row0;
 #pragma unroll
     for (int part = 0; part < 4; ++part)
@@ -333,7 +363,8 @@ __device__ __forceinline__ void rows_pass(const PassParams& p, unsigned char* ri
       for (int j = 0; j < C::NLOAD; ++j) {
         int r = min(64 * part + ld_row[j], qvalid - 1);
         if constexpr (kHeads) r = group_row(row0 + r) - at;
-        dma16(qg, (uint32_t)(r * C::ROWB + ck[j] * 16), ring_base + C::QOFF + part * C::OPB + wave * 1024 + j * 4096);
+        if constexpr (kShared) r = shared_row_offset(p, row0, row0 + r);
+        dma16(qg, kShared ? (uint32_t)r * C::ROWB + ck[j] * 16 : (uint32_t)(r * C::ROWB + ck[j] * 16), ring_base + C::QOFF + part * C::OPB + wave * 1024 + j * 4096);
       }
   }
   if (ntiles > 0) {
@@ -666,7 +697,8 @@ __device__ __forceinline__ void rows_pass(const PassParams& p, unsigned char* ri
     } else if (row_ok) {
       // (a branch of its own down to the stores: sharing them with the final partial's costs them their non-temporal hint, and these
       // partials, read once by the combine, then displace K and V in L2)
-      const size_t wrow = ((size_t)(split * p.B + b) * (kHeads ? p.heads_cap : p.Hkv) + (kHeads ? rank : kvh)) * nrows + row;
+      const size_t wrow = kShared ? (size_t)split * p.Hkv * nrows + shared_row(p, kvh, row)
+                                  : ((size_t)(split * p.B + b) * (kHeads ? p.heads_cap : p.Hkv) + (kHeads ? rank : kvh)) * nrows + row;
       float* __restrict__ w_o = own_block ? p.ws_o2 : p.ws_o;
 #pragma unroll
       for (int db = 0; db < C::NDB; ++db)

@@ -387,10 +387,11 @@ __device__ __forceinline__ void halves_pass(const PassParams& p, unsigned char* 
   static_assert(!PARTS || (MODE == kPassDense && (LAYOUT == kKeySplit || LAYOUT == kTileSplit)), "reference segments: dense pass");
   constexpr int NSETS = (MODE == kPassSparseRefresh) ? 2 : 1;
   using C = SCfg<D, LAYOUT, NSETS, NRG>;
-  static_assert(MODE == kPassDense || MODE == kPassDenseHeads || MODE == kPassDensePaged || MODE == kPassSparseReuse ||
+  static_assert(MODE == kPassDense || MODE == kPassDenseHeads || MODE == kPassDensePaged || MODE == kPassShared || MODE == kPassSparseReuse ||
                     MODE == kPassSparseRefresh || (MODE == kPassInternal && LAYOUT == kTileSplit), "modes of this form");
   constexpr bool kHalves = LAYOUT != kRowPairShort;
-  static_assert(kHalves || MODE == kPassDense, "one wavefront per row group: dense pass");
+  static_assert(kHalves || MODE == kPassDense || MODE == kPassShared, "one wavefront per row group: dense pass");
+  constexpr bool kPages = MODE == kPassDensePaged || MODE == kPassShared;      // keys in pages of a pool
   // Whole tiles and head_dim 64: two tiles per barrier (tiles t, t+1 are computed while t+2, t+3 are in flight); key split at 128:
   // one tile per barrier, NS - 1 in flight.
   constexpr bool kPairs = !key_split(LAYOUT) || paired_halves(D, LAYOUT);
@@ -475,9 +476,9 @@ __device__ __forceinline__ void halves_pass(const PassParams& p, unsigned char* 
   }
   // contiguous cache: this KV head's [nkeys, D] slab; paged cache: the pool (tiles add their page offset)
   const unsigned char* __restrict__ Kg =
-      (const unsigned char*)p.k + ((MODE == kPassDensePaged) ? (size_t)0 : (size_t)bk * nkeys * C::ROWB);
+      (const unsigned char*)p.k + (kPages ? (size_t)0 : (size_t)bk * nkeys * C::ROWB);
   const unsigned char* __restrict__ Vg =
-      (const unsigned char*)p.v + ((MODE == kPassDensePaged) ? (size_t)0 : (size_t)bk * nkeys * C::ROWB);
+      (const unsigned char*)p.v + (kPages ? (size_t)0 : (size_t)bk * nkeys * C::ROWB);
 
   // ---- tile list of this workgroup: a contiguous range of the pass's tile list, visited in rotated order
   // (workgroups that run in lockstep would otherwise read the same offset of their chunks, i.e. the same
@@ -611,7 +612,7 @@ __device__ __forceinline__ void halves_pass(const PassParams& p, unsigned char* 
       r.mask = (uint32_t)sload(umask, blk_i);
     } else if constexpr (MODE == kPassSparseRefresh) {
       r.mask = (uint32_t)sload(bmask, (int)fastdiv((uint32_t)r.e, p.div_tpb));
-    } else if constexpr (MODE == kPassDensePaged) {
+    } else if constexpr (kPages) {                              // (kPassShared: b is 0)
       r.word = sload(p.block_table + (size_t)b * p.max_pages, (int)fastdiv((uint32_t)(r.e * C::KT), p.div_page));
     }
     return r;
@@ -622,7 +623,7 @@ __device__ __forceinline__ void halves_pass(const PassParams& p, unsigned char* 
     d.k0 = (MODE == kPassSparseReuse)
                ? r.word * p.key_block + C::KT * (r.e - (int)(fastdiv((uint32_t)r.e, p.div_tpb) * p.div_tpb.d))
                : r.e * C::KT;
-    if constexpr (MODE == kPassDensePaged) {
+    if constexpr (kPages) {
       const uint32_t slot = fastdiv((uint32_t)d.k0, p.div_page);
       const int page = min(max(r.word, 0), p.num_pages - 1);       // clamped into the pool
       const int in_page = d.k0 - (int)(slot * p.div_page.d);
@@ -684,15 +685,16 @@ __device__ __forceinline__ void halves_pass(const PassParams& p, unsigned char* 
   // ---- prologue: the query rows go through the last ring stage(s), then the first tiles; everything is in
   // flight before the first wait.
   {
-    const unsigned char* qg = (const unsigned char*)p.q + (grow_base + row0) * C::ROWB;
+    const unsigned char* qg = (const unsigned char*)p.q + (MODE == kPassShared ? shared_row(p, kvh, row0) : grow_base + row0) * C::ROWB;
     const int qvalid = nrows - row0;                     // >= 1
     const uint32_t qbase = ring_base + (uint32_t)(C::NS - C::QSTAGES) * C::STAGE + wave * 1024;
 #pragma unroll
     for (int part = 0; part < C::QPARTS; ++part)         // 64 rows at a time, each laid out like a K operand
 #pragma unroll
       for (int j = 0; j < C::NLOAD; ++j) {
-        const int r = min(64 * part + ld_row[j], qvalid - 1);
-        dma16(qg, (uint32_t)(r * C::ROWB + ck[j] * 16), qbase + part * C::OPB + j * C::LSTEP);
+        int r = min(64 * part + ld_row[j], qvalid - 1);
+        if constexpr (MODE == kPassShared) r = shared_row_offset(p, row0, row0 + r);
+        dma16(qg, MODE == kPassShared ? (uint32_t)r * C::ROWB + ck[j] * 16 : (uint32_t)(r * C::ROWB + ck[j] * 16), qbase + part * C::OPB + j * C::LSTEP);
       }
   }
   constexpr int kPre = (AHEAD < C::NS - C::QSTAGES) ? AHEAD : C::NS - C::QSTAGES;   // tiles issued while the queries sit in the ring
@@ -1046,7 +1048,8 @@ __device__ __forceinline__ void halves_pass(const PassParams& p, unsigned char* 
       return;
     }
     if (!row_ok) return;
-    const size_t wrow = ((size_t)(split * p.B + b) * p.Hkv + kvh) * nrows + row;
+    const size_t wrow = MODE == kPassShared ? (size_t)split * p.Hkv * nrows + shared_row(p, kvh, row)
+                                            : ((size_t)(split * p.B + b) * p.Hkv + kvh) * nrows + row;
 #pragma unroll
     for (int i = 0; i < NSETS; ++i) {
       float* __restrict__ w_o = i ? p.ws_o2 : p.ws_o;
@@ -1103,8 +1106,8 @@ hipError_t launch_stream(const PassParams& p, hipStream_t s) {
   if (MODE == kPassRefreshFused && p.k2 != nullptr) nwg += (long long)p.B * p.Hkv * ntile_rows * 2;
   if (nwg >= (1ll << 31)) return hipErrorInvalidValue;
   PassParams q = p;
-  if (MODE == kPassDensePaged) q.div_page = make_fastdiv((uint32_t)p.page_size);
-  q.div_tpb = make_fastdiv((uint32_t)((MODE == kPassDenseHeads && LAYOUT == kRowPair) ? p.Bq : p.key_block > 0 ? p.key_block / kKeyTile : 1));
+  if (MODE == kPassDensePaged || MODE == kPassShared) q.div_page = make_fastdiv((uint32_t)p.page_size);
+  q.div_tpb = make_fastdiv((uint32_t)(MODE == kPassShared ? p.key_block : (MODE == kPassDenseHeads && LAYOUT == kRowPair) ? p.Bq : p.key_block > 0 ? p.key_block / kKeyTile : 1));
   {
     // long streams only: below 64 tiles per split a 1/64 bias rounds away
     const int tiles = (p.nkeys + kKeyTile - 1) / kKeyTile;
@@ -1213,6 +1216,9 @@ hipError_t launch_stream_d(const PassParams& p, PassMode mode, hipStream_t s) {
         default: return launch_stream<D, kPassInternal, kRowPair>(p, s);
       }
     case kPassRefreshFused: return launch_stream<D, kPassRefreshFused, kRowPair>(p, s);
+    case kPassShared:
+      if (nrows <= kRowsPerWgBf16) return launch_key_split<D, kPassShared>(p, s);
+      return short_row_pairs(p) ? launch_stream<D, kPassShared, kRowPairShort>(p, s) : launch_stream<D, kPassShared, kRowPair>(p, s);
     default: return hipErrorInvalidValue;
   }
 }
@@ -1241,6 +1247,7 @@ bool stream_bf16_covers(const PassParams& p, int D, PassMode mode) {
       // 158 and 39.9 / 65.1 / 141 / 155; one round, 32 heads of 1024 / 1536 rows 40.7 / 53.7 and 38.9 / 52.0).
       return internal_streams(p, D) > 0 || (internal_many_rows(p) && tiles >= 16);
     case kPassRefreshFused: return p.by_parity != 0;
+    case kPassShared: return true;
     default: return false;
   }
 }

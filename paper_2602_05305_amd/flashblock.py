@@ -95,6 +95,11 @@ _SIGNATURES = {
     "fb_rotate_block": (c_int, [POINTER(fb_shape), POINTER(fb_rotary), c_int32] + [POINTER(fb_rows)] * 6 + [c_void_p]),
     "fb_append_paged": (c_int, [POINTER(fb_shape), POINTER(fb_paged_kv), POINTER(fb_rotary), POINTER(fb_rows), POINTER(fb_rows), c_void_p,
                                 POINTER(fb_rows), POINTER(fb_rows), c_void_p, c_void_p]),
+    "fb_shared_workspace_bytes": (c_size_t, [POINTER(fb_shape), c_int32]),
+    "fb_external_partial_shared": (c_int, [POINTER(fb_shape), c_void_p, POINTER(fb_paged_kv), c_void_p, c_int32] + [c_void_p] * 4
+                                   + [c_size_t, c_void_p]),
+    "fb_refresh_step_shared": (c_int, [POINTER(fb_shape), c_void_p, POINTER(fb_paged_kv), c_void_p, c_int32] + [c_void_p] * 8
+                               + [c_size_t, c_void_p]),
 }
 
 
@@ -378,6 +383,24 @@ def fb_append_paged(shape, kv, rotary, k, v, append_lens=None, q=None, q_out=Non
     _check(st, "fb_append_paged")
 
 
+def fb_shared_workspace_bytes(shape, shared_len) -> int:
+    return int(load_library().fb_shared_workspace_bytes(ctypes.byref(shape), shared_len))
+
+
+def fb_external_partial_shared(shape, q, kv, shared_pages, shared_len, o_part, m_part, lse_part, workspace, stream=None):
+    st = load_library().fb_external_partial_shared(_ref(shape), _ptr(q), _ref(kv), _ptr(shared_pages), shared_len, _ptr(o_part), _ptr(m_part),
+                                                   _ptr(lse_part), _ptr(workspace), _nbytes(workspace), _stream(stream))
+    _check(st, "fb_external_partial_shared")
+
+
+def fb_refresh_step_shared(shape, q, kv, shared_pages, shared_len, k_block, v_block, o_part, m_part, lse_part, out, lse_out, workspace,
+                           stream=None):
+    st = load_library().fb_refresh_step_shared(_ref(shape), _ptr(q), _ref(kv), _ptr(shared_pages), shared_len, _ptr(k_block), _ptr(v_block),
+                                               _ptr(o_part), _ptr(m_part), _ptr(lse_part), _ptr(out), _ptr(lse_out), _ptr(workspace),
+                                               _nbytes(workspace), _stream(stream))
+    _check(st, "fb_refresh_step_shared")
+
+
 # The entry points in native form: what each C argument is made of, in C order (fb_call.c), and where the Python order differs.  The
 # functions above stay the definition of arguments and defaults, and take what the native form does not.  (A call's marshalling 1.4 -> 0.5 us.)
 _KINDS = {
@@ -399,6 +422,8 @@ _KINDS = {
 _CACHE_KINDS = {
     "fb_rotate_block": ("STIRRRRRRH", "shape rotary inverse q k v q_out k_out v_out stream"),
     "fb_append_paged": "SKTRRPRRPH",
+    "fb_external_partial_shared": "SPKPIPPPWH",
+    "fb_refresh_step_shared": "SPKPIPPPPPPPWH",
 }
 
 

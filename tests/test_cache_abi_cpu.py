@@ -161,3 +161,45 @@ def test_views_that_are_none_are_refused():
         fb.fb_rotate_block(bad, _rotary(), Tensor(), None, None, Tensor(), None, None, stream=0)
     with pytest.raises(ValueError):
         fb.make_rotary(Tensor(), [])
+
+
+def _shared(shape=None, q=FAKE, kv=0, pages=FAKE, shared_len=1000, o=FAKE, m=FAKE, lse=FAKE, ws=FAKE, nbytes=1 << 40, step=None):
+    lib, shape = fb.load_library(), shape or _shape()
+    kv = _paged() if kv == 0 else kv
+    if step is None:
+        return lib.fb_external_partial_shared(_ref(shape), q, _ref(kv), pages, shared_len, o, m, lse, ws, nbytes, None)
+    kb, vb, out, lse_out = step
+    return lib.fb_refresh_step_shared(_ref(shape), q, _ref(kv), pages, shared_len, kb, vb, o, m, lse, out, lse_out, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(q=None), fb.FB_ERR_NULL), (dict(kv=None), fb.FB_ERR_NULL), (dict(o=None), fb.FB_ERR_NULL), (dict(m=None), fb.FB_ERR_NULL), (dict(lse=None), fb.FB_ERR_NULL),
+    (dict(pages=None), fb.FB_ERR_NULL), (dict(kv=_paged(block_table=None)), fb.FB_ERR_NULL), (dict(kv=_paged(prefix_lens=None)), fb.FB_ERR_NULL),
+    (dict(kv=_paged(k_pool=None)), fb.FB_ERR_NULL), (dict(kv=_paged(v_pool=None)), fb.FB_ERR_NULL),
+    (dict(shared_len=-1), fb.FB_ERR_SHAPE), (dict(shared_len=(1 << 30) + 1), fb.FB_ERR_UNSUPPORTED), (dict(kv=_paged(struct_size=1)), fb.FB_ERR_SHAPE),
+    (dict(kv=_paged(num_pages=0)), fb.FB_ERR_SHAPE), (dict(kv=_paged(page_size=0)), fb.FB_ERR_SHAPE), (dict(kv=_paged(max_pages=0)), fb.FB_ERR_SHAPE),
+    (dict(kv=_paged(page_size=96)), fb.FB_ERR_UNSUPPORTED), (dict(kv=_paged(max_pages=1)), fb.FB_ERR_SHAPE),
+    (dict(q=ODD), fb.FB_ERR_ALIGN), (dict(o=ODD), fb.FB_ERR_ALIGN), (dict(ws=ODD), fb.FB_ERR_ALIGN), (dict(kv=_paged(v_pool=ODD)), fb.FB_ERR_ALIGN),
+    (dict(pages=FAKE + 2), fb.FB_ERR_ALIGN), (dict(ws=None), fb.FB_ERR_WORKSPACE), (dict(nbytes=64), fb.FB_ERR_WORKSPACE),
+    (dict(shape=_shape(head_dim=32)), fb.FB_ERR_UNSUPPORTED), (dict(shape=_shape(dtype=9)), fb.FB_ERR_DTYPE), (dict(shape=_shape(n_q_heads=3)), fb.FB_ERR_SHAPE),
+    (dict(shape=_shape(batch=2, n_q_heads=1 << 14, n_kv_heads=1 << 14, head_dim=128, block_len=1 << 13, prefix_len=0)), fb.FB_ERR_UNSUPPORTED),     # rows further than 32 bits apart
+])
+def test_shared_refusals(kw, status):
+    assert _shared(**kw) == status
+    assert _shared(**kw, step=(FAKE, FAKE, FAKE, None)) == status
+
+
+def test_shared_step_refusals():
+    for step, status in (((None, FAKE, FAKE, FAKE), fb.FB_ERR_NULL), ((FAKE, None, FAKE, FAKE), fb.FB_ERR_NULL), ((FAKE, FAKE, None, FAKE), fb.FB_ERR_NULL),
+                         ((ODD, FAKE, FAKE, FAKE), fb.FB_ERR_ALIGN), ((FAKE, FAKE, ODD, FAKE), fb.FB_ERR_ALIGN), ((FAKE, FAKE, FAKE, ODD), fb.FB_ERR_ALIGN)):
+        assert _shared(step=step) == status
+
+
+def test_shared_workspace_query():
+    s = _shape()
+    assert fb.fb_shared_workspace_bytes(s, 0) >= 2 * 4 * 3 * 66 * 4
+    assert fb.fb_shared_workspace_bytes(s, 1 << 20) > fb.fb_shared_workspace_bytes(s, 64)
+    assert fb.fb_shared_workspace_bytes(_shape(prefix_len=0), 0) >= 256
+    assert fb.fb_shared_workspace_bytes(s, -1) == 0 and fb.fb_shared_workspace_bytes(_shape(batch=0), 64) == 0 and fb.fb_shared_workspace_bytes(s, (1 << 30) + 1) == 0
+    n = fb.fb_shared_workspace_bytes(s, 1000)
+    assert _shared(nbytes=n - 1) == fb.FB_ERR_WORKSPACE
