@@ -23,7 +23,7 @@ CALIB_LIB = os.path.join(HERE, "libfbcalib.so")
 # host code only: the binding's native marshalling.  Named for the interpreter it is compiled for: another one does not load it.
 CALL_LIB = os.path.join(HERE, "_fbcall" + sysconfig.get_config_var("EXT_SUFFIX"))
 CALIB_SOURCES = ["fb_calib.hip"]
-SOURCES = ["fb_api.hip", "fb_attn_f32.hip", "fb_attn_bf16.hip", "fb_stream_bf16.hip", "fb_aux.hip", "fb_rotary.hip"]
+SOURCES = ["fb_api.hip", "fb_attn_f32.hip", "fb_attn_bf16.hip", "fb_stream_bf16.hip", "fb_aux.hip", "fb_rotary.hip", "fb_finish_bf16.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # the direct-to-LDS loads set M0 from inline assembly and say so in the clobber list

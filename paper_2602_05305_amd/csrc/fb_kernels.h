@@ -230,6 +230,22 @@ struct RotateParams {
   int max_pages, num_pages, capacity;
 };
 
+// Second launch over a shared prefix (fb_finish_bf16.hip): the fold of nsplit split partials, the own keys if own_keys > 0 (a sequence's
+// largest number of them), and with k_block != null the block of at most kFinishBlock rows and the merge.
+constexpr int kFinishBlock = 32;
+constexpr int kFinishRound = 512;      // its workgroups on the chip at once
+struct FinishParams {
+  const void* q; const void* k_pool; const void* v_pool; const void* k_block; const void* v_block;
+  const int32_t* block_table; const int32_t* prefix_lens;
+  const float* ws_o; const float* ws_m; const float* ws_l;
+  float* o; float* m; float* lse; void* out; float* lse_out;
+  long long rows;              // of a split
+  int nsplit, B, Hq, Hkv, G, Bq, own_keys, page_size, max_pages, num_pages;
+  const int32_t* order;        // sequences as workgroups take them, or null
+  float scale_log2;
+  FastDiv div_rowtiles, div_hkv, div_page;
+};
+
 // Host-side launchers; each returns the hipError_t of its launch(es).
 hipError_t launch_attn_f32(const PassParams& p, int D, PassMode mode, hipStream_t s);
 hipError_t launch_attn_bf16(const PassParams& p, int D, PassMode mode, hipStream_t s);
@@ -237,6 +253,11 @@ hipError_t launch_attn_bf16(const PassParams& p, int D, PassMode mode, hipStream
 bool stream_bf16_covers(const PassParams& p, int D, PassMode mode);
 hipError_t launch_stream_bf16(const PassParams& p, int D, PassMode mode, hipStream_t s);
 int stream_bf16_name(const PassParams& p, int D, PassMode mode, char* buf, size_t n);
+// kPassShared and, if own.nsplit > 0, kPassDensePaged over the sequences' own keys, in one launch; order != null: gets the sequences by
+// descending own.prefix_lens.
+// Rows of a workgroup (256: of 8 wavefronts of 32 rows, or of 4 of 64, which needs kRowsTiles tiles to a split).
+enum SharedRows : int { kShared32, kShared64, kShared128, kShared256Short, kShared256 };
+hipError_t launch_shared_bf16(const PassParams& shared, const PassParams& own, int32_t* order, SharedRows rows, int D, hipStream_t s);
 // Whether the internal pass of p can fold p.fold_ns split partials itself (few splits; not the row-pair kernels).
 bool internal_fold_covers(const PassParams& p, int D);
 // Name of the kernel launch_attn_bf16 runs for the dense external pass of p (profiler spelling, no namespace).
@@ -254,6 +275,7 @@ hipError_t launch_block_mass_f32(const MassParams& p, int D, hipStream_t s);
 hipError_t launch_block_mass_bf16(const MassParams& p, int D, hipStream_t s);
 hipError_t launch_seq_order(const int32_t* prefix_lens, int32_t* seq_order, int B, hipStream_t s);
 hipError_t launch_head_similarity(const float* o_a, const float* o_b, float* sim, int BH, int Bq, int D, hipStream_t s);
+hipError_t launch_shared_finish(const FinishParams& p, int D, hipStream_t s);
 hipError_t launch_rotate(const RotateParams& p, int D, bool is_bf16, hipStream_t s);
 
 // Row tiles (workgroups along the group-flattened row axis) per KV group, per kernel family.

@@ -118,7 +118,7 @@ __device__ __forceinline__ void dma16_at(const void* base, uint32_t off, uint32_
 }
 
 template <int D, int MODE>
-__device__ __forceinline__ void rows_pass(const PassParams& p, unsigned char* ring) {
+__device__ __forceinline__ void rows_pass(const PassParams& p, unsigned char* ring, uint32_t wg, uint32_t nwgs) {
   using C = RCfg<D>;
   constexpr bool kHeads = MODE == kPassDenseHeads;
   // refresh step in several splits: every split as two streams (below), and two more over the block's own keys
@@ -129,9 +129,9 @@ __device__ __forceinline__ void rows_pass(const PassParams& p, unsigned char* ri
 
   // ---- workgroup -> (row tile, batch, KV head, split): a contiguous range of units per XCD (fb_stream_bf16.hip); per-head
   // refresh: whole heads drop out, so a head's row tiles are dealt over the XCDs
-  const int nwg = gridDim.x;
+  const int nwg = nwgs;
   const int nrows = p.G * p.Bq;
-  int w = blockIdx.x;
+  int w = wg;
   bool own_block = false;                                    // (the prefix's workgroups are the first of the grid)
   if constexpr (!kHeads) {
     const int npre = kFused ? p.B * p.Hkv * p.nsplit * (int)p.div_rowtiles.d : nwg;
@@ -227,7 +227,7 @@ __device__ __forceinline__ void rows_pass(const PassParams& p, unsigned char* ri
   // whose references these are)
   const int total = (nkeys + C::KT - 1) / C::KT;
   TileRange tr = (MODE == kPassInternal) ? TileRange{0, total} : split_range(total, p.div_nsplit, split);
-  uint32_t rsrc = (p.div_rowtiles.d == 1) ? blockIdx.x : unit;
+  uint32_t rsrc = (p.div_rowtiles.d == 1) ? wg : unit;
   int stride = 1, first = 0;
   if constexpr (kFused) {
     const int pairs = p.nsplit / 2, range_i = own_block ? pairs - 1 : split >> 1;

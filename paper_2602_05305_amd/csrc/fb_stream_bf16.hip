@@ -382,8 +382,9 @@ constexpr uint32_t kSegFirst = 1u, kSegReference = 2u, kSegPad = 4u;
 
 // Every layout but kRowPair: two wavefronts per row group, or one (kRowPairShort).  PARTS: the stream of a (batch element, KV head) is
 // p.nseg reference segments, each visited in an order of its own, and the workgroups take p.nsplit even pieces of that walk.
-template <int D, int MODE, int LAYOUT, int NRG, bool PARTS>
-__device__ __forceinline__ void halves_pass(const PassParams& p, unsigned char* ring) {
+// wg, nwgs: this workgroup of those of the pass.  ORDER: the paged pass may rank the sequences by length.
+template <int D, int MODE, int LAYOUT, int NRG, bool PARTS, bool ORDER = true>
+__device__ __forceinline__ void halves_pass(const PassParams& p, unsigned char* ring, uint32_t wg, uint32_t nwgs) {
   static_assert(!PARTS || (MODE == kPassDense && (LAYOUT == kKeySplit || LAYOUT == kTileSplit)), "reference segments: dense pass");
   constexpr int NSETS = (MODE == kPassSparseRefresh) ? 2 : 1;
   using C = SCfg<D, LAYOUT, NSETS, NRG>;
@@ -405,19 +406,19 @@ __device__ __forceinline__ void halves_pass(const PassParams& p, unsigned char* 
 
   // ---- workgroup -> (row tile, batch, KV head, split).  Hardware deals consecutive workgroup ids round-robin
   // to the 8 XCDs; each XCD gets a contiguous range of units so that row tiles sharing K/V share an L2.
-  const int nwg = gridDim.x;
+  const int nwg = nwgs;
   const int nrows = p.G * p.Bq;
   int rt;
   uint32_t rest;
   if constexpr (MODE == kPassDensePaged) {
     // ragged sequences: contiguous ranges would give the XCDs unequal work; deal the units round-robin
-    const uint32_t j = blockIdx.x >> 3, xcd = blockIdx.x & 7;
+    const uint32_t j = wg >> 3, xcd = wg & 7;
     const uint32_t jq = fastdiv(j, p.div_rowtiles);
     rt = (int)(j - jq * p.div_rowtiles.d);
     rest = jq * 8 + xcd;
     if (rest >= (uint32_t)(p.B * p.Hkv * p.nsplit)) return;   // workgroup-uniform
   } else {
-    const int bid = blockIdx.x, q8 = nwg / 8, r8 = nwg % 8;
+    const int bid = wg, q8 = nwg / 8, r8 = nwg % 8;
     const int xcd = bid % 8, j = bid / 8;
     int w = (xcd < r8 ? xcd * (q8 + 1) : r8 * (q8 + 1) + (xcd - r8) * q8) + j;
     // biased cut (the host sets it only for one row tile, an even split count and a grid that is a multiple of 8):
@@ -436,7 +437,7 @@ __device__ __forceinline__ void halves_pass(const PassParams& p, unsigned char* 
   rest = r2;
   int b = (int)fastdiv(rest, p.div_hkv);
   const int kvh = (int)(rest - (uint32_t)b * p.div_hkv.d);
-  if constexpr (MODE == kPassDensePaged) {
+  if constexpr (MODE == kPassDensePaged && ORDER) {
     if (p.seq_order != nullptr) {
       b = sload(p.seq_order, b);
     } else if (p.order_inline) {
@@ -491,7 +492,7 @@ __device__ __forceinline__ void halves_pass(const PassParams& p, unsigned char* 
     total = (nkeys + C::KT - 1) / C::KT;
   }
   TileRange tr = p.xcd_bias ? biased_range(total, p.div_bias, split) : split_range(total, p.div_nsplit, split);
-  const uint32_t rsrc = (p.div_rowtiles.d == 1) ? blockIdx.x : unit;
+  const uint32_t rsrc = (p.div_rowtiles.d == 1) ? wg : unit;
   if constexpr (LAYOUT == kTileSplit) {
     // as the register-staged refresh pass cuts them, so that the running references start from the same tiles and results
     // stay the same up to fp32 sums: the last split is blk_cost tiles (at most half a split, 3 for a block of one tile) shorter
@@ -1078,13 +1079,17 @@ __device__ __forceinline__ void halves_pass(const PassParams& p, unsigned char* 
 template <int D, int MODE, int LAYOUT, int NRG>
 __global__ __launch_bounds__(LAYOUT == kRowPair ? RCfg<D>::THREADS : LAYOUT == kRowPairShort ? 512 : 2 * NRG * 64, 1) void attn_stream_kernel(const PassParams p) {
   extern __shared__ __align__(16) unsigned char ring[];
-  if constexpr (LAYOUT == kRowPair) rows_pass<D, MODE>(p, ring);
-  else halves_pass<D, MODE, whole_layout(LAYOUT), NRG, in_parts(LAYOUT)>(p, ring);
+  if constexpr (LAYOUT == kRowPair) rows_pass<D, MODE>(p, ring, blockIdx.x, gridDim.x);
+  else halves_pass<D, MODE, whole_layout(LAYOUT), NRG, in_parts(LAYOUT)>(p, ring, blockIdx.x, gridDim.x);
 }
 
-template <int D, int MODE, int LAYOUT, int NRG = 4>
-hipError_t launch_stream(const PassParams& p, hipStream_t s) {
-  using C = std::conditional_t<LAYOUT == kRowPair, RCfg<D>, SCfg<D, whole_layout(LAYOUT), (MODE == kPassSparseRefresh) ? 2 : 1, NRG>>;
+template <int D, int MODE, int LAYOUT, int NRG>
+using LayoutCfg = std::conditional_t<LAYOUT == kRowPair, RCfg<D>, SCfg<D, whole_layout(LAYOUT), (MODE == kPassSparseRefresh) ? 2 : 1, NRG>>;
+
+// The parameters a pass is launched with, in q, and its workgroups.
+template <int D, int MODE, int LAYOUT, int NRG>
+hipError_t stream_grid(const PassParams& p, PassParams& q, long long& nwg) {
+  using C = LayoutCfg<D, MODE, LAYOUT, NRG>;
   // row pairs: the shortest range has to hold what is loaded ahead (the routes here ask for more); per-head refresh: two splits
   // share a range
   if (LAYOUT == kRowPair && (p.nkeys + C::KT - 1) / C::KT < kRowsTiles * (MODE == kPassDenseHeads || MODE == kPassRefreshFused ? (p.nsplit + 1) / 2 : p.nsplit))
@@ -1094,18 +1099,14 @@ hipError_t launch_stream(const PassParams& p, hipStream_t s) {
     const int pairs = p.nsplit / 2, tiles = (p.nkeys + C::KT - 1) / C::KT, all = tiles + p.blk_cost;
     if (p.nsplit % 2 != 0 || pairs < 1 || all / pairs - p.blk_cost < kRowsTiles || (p.k2 != nullptr && (p.Bq + C::KT - 1) / C::KT < kRowsTiles)) return hipErrorInvalidValue;
   }
-  auto kern = attn_stream_kernel<D, MODE, LAYOUT, NRG>;
-  static LdsLimit lim;
-  hipError_t e = raise_lds_limit(kern, C::LDS, lim, C::LDS);
-  if (e != hipSuccess) return e;
   const int nrows = p.G * p.Bq;
   const int ntile_rows = (nrows + C::ROWS - 1) / C::ROWS;
-  long long nwg = (long long)p.B * p.Hkv * ntile_rows * p.nsplit;
+  nwg = (long long)p.B * p.Hkv * ntile_rows * p.nsplit;
   if (MODE == kPassDensePaged) nwg = (((long long)p.B * p.Hkv * p.nsplit + 7) / 8) * 8 * ntile_rows;
   if (MODE == kPassDenseHeads && LAYOUT == kRowPair) nwg = (long long)p.B * (p.heads_cap * p.nsplit + p.Hkv) * ntile_rows;
   if (MODE == kPassRefreshFused && p.k2 != nullptr) nwg += (long long)p.B * p.Hkv * ntile_rows * 2;
   if (nwg >= (1ll << 31)) return hipErrorInvalidValue;
-  PassParams q = p;
+  q = p;
   if (MODE == kPassDensePaged || MODE == kPassShared) q.div_page = make_fastdiv((uint32_t)p.page_size);
   q.div_tpb = make_fastdiv((uint32_t)(MODE == kPassShared ? p.key_block : (MODE == kPassDenseHeads && LAYOUT == kRowPair) ? p.Bq : p.key_block > 0 ? p.key_block / kKeyTile : 1));
   {
@@ -1129,7 +1130,80 @@ hipError_t launch_stream(const PassParams& p, hipStream_t s) {
   q.div_rowtiles = make_fastdiv((uint32_t)ntile_rows);
   q.div_nsplit = make_fastdiv((uint32_t)p.nsplit);
   q.div_hkv = make_fastdiv((uint32_t)p.Hkv);
+  return hipSuccess;
+}
+
+template <int D, int MODE, int LAYOUT, int NRG = 4>
+hipError_t launch_stream(const PassParams& p, hipStream_t s) {
+  using C = LayoutCfg<D, MODE, LAYOUT, NRG>;
+  PassParams q;
+  long long nwg = 0;
+  hipError_t e = stream_grid<D, MODE, LAYOUT, NRG>(p, q, nwg);
+  if (e != hipSuccess) return e;
+  auto kern = attn_stream_kernel<D, MODE, LAYOUT, NRG>;
+  static LdsLimit lim;
+  e = raise_lds_limit(kern, C::LDS, lim, C::LDS);
+  if (e != hipSuccess) return e;
   launch_attn_kernel(kern, dim3((unsigned)nwg), dim3(C::THREADS), C::LDS, s, q);
+  return hipGetLastError();
+}
+
+// Shared prefix: the pass over the shared keys, in any layout, and the paged pass over the sequences' own keys in one grid.  The own keys'
+// workgroups come last: they take the compute units that the shared ones leave, and then the whole chip.
+struct SharedParams {
+  PassParams shared, own;      // own.nsplit == 0: none
+  uint32_t shared_wgs;
+  const int32_t* lens; int32_t* order; int sequences;      // order != null: the next launch wants the sequences by length
+};
+constexpr int own_groups(int layout, int nrg) { return layout == kRowPair ? 2 : layout == kRowPairShort ? 4 : nrg; }
+
+template <int D, int LAYOUT, int NRG>
+__global__ __launch_bounds__(LAYOUT == kRowPair ? RCfg<D>::THREADS : LAYOUT == kRowPairShort ? 512 : 2 * NRG * 64, 1) void attn_shared_kernel(const SharedParams p) {
+  extern __shared__ __align__(16) unsigned char ring[];
+  if (blockIdx.x >= p.shared_wgs) {
+    halves_pass<D, kPassDensePaged, kKeySplit, own_groups(LAYOUT, NRG), false, false>(p.own, ring, blockIdx.x - p.shared_wgs, gridDim.x - p.shared_wgs);
+  } else {
+    if constexpr (LAYOUT == kRowPair) rows_pass<D, kPassShared>(p.shared, ring, blockIdx.x, p.shared_wgs);
+    else halves_pass<D, kPassShared, LAYOUT, NRG, false>(p.shared, ring, blockIdx.x, p.shared_wgs);
+  }
+  if (p.order != nullptr && threadIdx.x < 64) {
+    // the rank of a sequence for every workgroup, the longest first, ties: the lower index
+    const int lane = threadIdx.x;
+    for (int i = blockIdx.x; i < p.sequences; i += gridDim.x) {
+      const int mine = p.lens[i];
+      int rank = 0;
+      for (int j0 = 0; j0 < p.sequences; j0 += 64) {
+        const int j = j0 + lane, other = p.lens[min(j, p.sequences - 1)];
+        rank += __popcll(__ballot(j < p.sequences && (other > mine || (other == mine && j < i))));
+      }
+      if (lane == 0) p.order[rank] = i;
+    }
+  }
+}
+
+template <int D, int LAYOUT, int NRG = 4>
+hipError_t launch_shared(const PassParams& shared, const PassParams& own, int32_t* order, hipStream_t s) {
+  using C = LayoutCfg<D, kPassShared, LAYOUT, NRG>;
+  constexpr int OWN = own_groups(LAYOUT, NRG);
+  using O = SCfg<D, kKeySplit, 1, OWN>;
+  static_assert(O::THREADS == C::THREADS, "both passes in one grid");
+  SharedParams q;
+  long long nwg = 0, nown = 0;
+  hipError_t e = stream_grid<D, kPassShared, LAYOUT, NRG>(shared, q.shared, nwg);
+  if (e != hipSuccess) return e;
+  q.own = own;
+  if (own.nsplit > 0 && (e = stream_grid<D, kPassDensePaged, kKeySplit, OWN>(own, q.own, nown)) != hipSuccess) return e;
+  if (nwg + nown >= (1ll << 31)) return hipErrorInvalidValue;
+  q.shared_wgs = (uint32_t)nwg;
+  q.lens = own.prefix_lens;
+  q.order = order;
+  q.sequences = own.B;
+  constexpr size_t lds = C::LDS > O::LDS ? C::LDS : O::LDS;
+  auto kern = attn_shared_kernel<D, LAYOUT, NRG>;
+  static LdsLimit lim;
+  e = raise_lds_limit(kern, lds, lim, lds);
+  if (e != hipSuccess) return e;
+  launch_attn_kernel(kern, dim3((unsigned)(nwg + nown)), dim3(C::THREADS), lds, s, q);
   return hipGetLastError();
 }
 
@@ -1216,9 +1290,6 @@ hipError_t launch_stream_d(const PassParams& p, PassMode mode, hipStream_t s) {
         default: return launch_stream<D, kPassInternal, kRowPair>(p, s);
       }
     case kPassRefreshFused: return launch_stream<D, kPassRefreshFused, kRowPair>(p, s);
-    case kPassShared:
-      if (nrows <= kRowsPerWgBf16) return launch_key_split<D, kPassShared>(p, s);
-      return short_row_pairs(p) ? launch_stream<D, kPassShared, kRowPairShort>(p, s) : launch_stream<D, kPassShared, kRowPair>(p, s);
     default: return hipErrorInvalidValue;
   }
 }
@@ -1247,7 +1318,6 @@ bool stream_bf16_covers(const PassParams& p, int D, PassMode mode) {
       // 158 and 39.9 / 65.1 / 141 / 155; one round, 32 heads of 1024 / 1536 rows 40.7 / 53.7 and 38.9 / 52.0).
       return internal_streams(p, D) > 0 || (internal_many_rows(p) && tiles >= 16);
     case kPassRefreshFused: return p.by_parity != 0;
-    case kPassShared: return true;
     default: return false;
   }
 }
@@ -1259,6 +1329,22 @@ int stream_bf16_name(const PassParams& p, int D, PassMode mode, char* buf, size_
   return snprintf(buf, n, "attn_stream_kernel<%d, %d, %d, %d>", D, (int)mode,
                   !rp ? (int)(mode == kPassDense && p.nseg > 0 && p.nseg != p.nsplit ? kKeySplitParts : kKeySplit) : mode == kPassDense && short_row_pairs(p) ? (int)kRowPairShort : (int)kRowPair,
                   (rp || nrows > 64) ? 4 : nrows > 32 ? 2 : 1);
+}
+
+template <int D>
+hipError_t launch_shared_d(const PassParams& shared, const PassParams& own, int32_t* order, SharedRows rows, hipStream_t s) {
+  switch (rows) {
+    case kShared32: return launch_shared<D, kKeySplit, 1>(shared, own, order, s);
+    case kShared64: return launch_shared<D, kKeySplit, 2>(shared, own, order, s);
+    case kShared128: return launch_shared<D, kKeySplit, 4>(shared, own, order, s);
+    case kShared256Short: return launch_shared<D, kRowPairShort>(shared, own, order, s);
+    case kShared256: return launch_shared<D, kRowPair>(shared, own, order, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_shared_bf16(const PassParams& shared, const PassParams& own, int32_t* order, SharedRows rows, int D, hipStream_t s) {
+  return D == 64 ? launch_shared_d<64>(shared, own, order, rows, s) : launch_shared_d<128>(shared, own, order, rows, s);
 }
 
 hipError_t launch_stream_bf16(const PassParams& p, int D, PassMode mode, hipStream_t s) {
