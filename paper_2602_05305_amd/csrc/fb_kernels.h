@@ -217,11 +217,14 @@ struct RotatePart {
   int heads;
   int turned;                 // else the rows are only moved
   int paged;                  // dst is a pool [num_pages, heads, page_size, D]
+  int tokens_log2;            // tokens of a workgroup, set by the launcher like the next two: its first workgroup, its groups of heads
+  uint32_t first_wg;
+  FastDiv div_groups;
 };
 struct RotateParams {
   RotatePart part[3];
-  uint32_t tokens, head_groups;                // batch * block_len; workgroups along the heads
-  FastDiv div_block, div_page;
+  uint32_t tokens;                             // batch * block_len
+  FastDiv div_block, div_page, div_pairs;
   const float* inv_freq; const int32_t* positions; const int32_t* first;
   long long position_stride;
   int pairs, adjacent, inverse, n_axes, offset, axis_end[4];
