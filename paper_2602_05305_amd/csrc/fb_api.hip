@@ -1340,7 +1340,9 @@ fb_status shared_partials(const fb_shape* shape, const void* q, const fb_paged_k
   p.page_size = kv->page_size; p.max_pages = kv->max_pages; p.num_pages = kv->num_pages;
   hipError_t e = hipSuccess;
   own = plan.ns_own > 0;
-  if (own && shape->batch > 1 && (shape->dtype != FB_BF16 || plan.ns_shared == 0)) {
+  // (fp32 workgroups of one round need no order)
+  const long long own_wgs = (long long)shape->batch * shape->n_kv_heads * plan.ns_own * ((group + 15) / 16);
+  if (own && shape->batch > 1 && (shape->dtype == FB_BF16 ? plan.ns_shared == 0 : own_wgs > 256)) {
     if (shape->batch <= 128 && shape->dtype == FB_BF16) {
       p.order_inline = 1;
     } else {

@@ -7,10 +7,13 @@
 //   * A wavefront is by itself until the end: it loads tiles of 8 KB of keys and as much of values straight into its own LDS stage, waits
 //     for its own loads and computes all 32 rows with them, no workgroup barrier.  The four wavefronts take every fourth tile; eight of them to
 //     a CU (two workgroups) keep 128 KB in flight, three times what HBM asks of a CU, so a wavefront does not load ahead.
-//   * The block's own keys, at most 32, are one tile of the last wavefront, into accumulators of their own.
+//   * The block's own keys, at most 32, are one tile, the last wavefront's, which then takes none of the others: a second set of accumulators
+//     for it (255 registers instead of 206) made four wavefronts of own keys no faster than three.
 //   * Row groups of the same KV head come next to each other on one XCD, whose L2 serves the second and later readings of the keys.
 //   * At the end the wavefronts' sums meet in LDS, 64 columns at a time (so that it fits where the stages were).  A group of 8
-//     threads folds the split partials of a row, several groups where the workgroup has few rows, each every n-th split.
+//     threads folds the split partials of a row, several groups where the workgroup has few rows, each every n-th split; groups of a wavefront
+//     meet in registers.  Cycle stamps, batch 64, one row of 32 / 8 heads, head_dim 128, us: length and page 0.5, first tile 2.2, partials 0.4
+//     (16 splits 1.6), the end 1.8 (2.9 with LDS reads one after the other); own keys spread to 512, 67 MB, 8 at the median and 12 for the longest.
 // Tiles, rotations and register layouts are those of the streaming kernel (fb_stream_bf16.hip); sums and statistics are fp32, weights
 // are rounded to bf16 for the value product, as there.
 #include "fb_kernels.h"
@@ -29,7 +32,7 @@ struct NCfg {
   static constexpr int NLOAD = OPB / 1024;
   static constexpr int NKS = D / 16, NDB = D / 32;
   static constexpr int RS = 64 + 4;                           // floats of a row of 64 columns in LDS
-  static constexpr int RECS = kWaves + 2;                     // wavefronts, block, split partials
+  static constexpr int RECS = kWaves + 1;                     // wavefronts, split partials
   static constexpr int RING = kWaves * STAGE, REC = RECS * 32 * RS * 4;
   static constexpr int STAT = RING > REC ? RING : REC;        // then (m, l) of every record's rows
   static constexpr int LDS = STAT + RECS * 32 * 8;
@@ -52,18 +55,46 @@ struct FinAcc {
   }
 };
 
-// 8 columns of a partial, log2-domain reference, sum.
-struct Part8 {
-  f32x4 a, b;
+// What a thread folds of a row's split partials: 8 columns of each 64, log2-domain reference, sum.
+template <int NH>
+struct Folded {
+  f32x4 a[NH], b[NH];
   float m, l;
 };
-__device__ __forceinline__ void add_part(Part8& f, const f32x4& a, const f32x4& b, float l, float w) {
+// With the lanes across: of both sides the same row, one after the other.
+enum Across { kAcross32, kAcross16, kAcross8 };
+template <int NH, Across ACROSS>
+__device__ __forceinline__ void fold_lanes(Folded<NH>& f) {
+  auto both = [](float x, float& lo, float& hi) __attribute__((always_inline)) {
+    if constexpr (ACROSS == kAcross8) {
+      lo = x;
+      hi = turn16<8>(x);
+    } else if constexpr (ACROSS == kAcross16) {
+      const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+      lo = __uint_as_float(r[0]);
+      hi = __uint_as_float(r[1]);
+    } else {
+      const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+      lo = __uint_as_float(r[0]);
+      hi = __uint_as_float(r[1]);
+    }
+  };
+  float m0, m1, lo, hi;
+  both(f.m, m0, m1);
+  f.m = fmaxf(m0, m1);
+  const float mu = f.m == -INFINITY ? 0.f : f.m, w0 = __builtin_amdgcn_exp2f(m0 - mu), w1 = __builtin_amdgcn_exp2f(m1 - mu);
+  auto fold = [&](float x) __attribute__((always_inline)) {
+    both(x, lo, hi);
+    return fmaf(hi, w1, lo * w0);
+  };
+  f.l = fold(f.l);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f.a[i] = fmaf(a[i], w, f.a[i]);
-    f.b[i] = fmaf(b[i], w, f.b[i]);
-  }
-  f.l = fmaf(l, w, f.l);
+  for (int half = 0; half < NH; ++half)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f.a[half][i] = fold(f.a[half][i]);
+      f.b[half][i] = fold(f.b[half][i]);
+    }
 }
 
 template <int D>
@@ -109,19 +140,36 @@ __global__ __launch_bounds__(256, 2) void shared_finish_kernel(const FinishParam
       vaddr[db] = (uint32_t)(C::OPB + rrow * C::ROWB + ((4 * db + 2 * blk1 + ((i16 & 3) >> 1) + C::rot_v(rrow)) & (C::CPR - 1)) * 16 + (i16 & 1) * 8);
   }
 
+  // direct-to-LDS load j: LDS chunk 64 j + lane is row ROWS1 j + lane / CPR, position lane % CPR, and holds the row's chunk (position - rotation).
+  // Rotations come round in j, so the offsets of PK loads of keys and one of values are enough; the rest is in the scalar address.
+  constexpr int ROWS1 = 64 / C::CPR, PK = D == 128 ? 4 : 2;
+  const int lrow = lane / C::CPR, lpc = lane % C::CPR;
+  uint32_t off_k[PK];
+#pragma unroll
+  for (int j = 0; j < PK; ++j) off_k[j] = (uint32_t)(lrow * C::ROWB + ((lpc - C::rot_k(ROWS1 * j + lrow)) & (C::CPR - 1)) * 16);
+  const uint32_t off_v = (uint32_t)(lrow * C::ROWB + ((lpc - C::rot_v(lrow)) & (C::CPR - 1)) * 16);
+
   // one tile of this wavefront: nvalid of its keys exist
   auto tile = [&](FinAcc<C::NDB>& acc, const unsigned char* kt, const unsigned char* vt, int nvalid) __attribute__((always_inline)) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");        // the last tile's reads have left the stage
-    const int last = min(nvalid, C::KT) - 1;                  // rows past the end read the last key (their scores are masked)
+    const bool ragged = nvalid < C::KT;                       // wavefront-uniform
+    if (!ragged) {
 #pragma unroll
-    for (int j = 0; j < C::NLOAD; ++j) {
-      const int c = j * 64 + lane, r = c / C::CPR, pc = c % C::CPR;
-      dma16(kt, (uint32_t)(min(r, last) * C::ROWB + ((pc - C::rot_k(r)) & (C::CPR - 1)) * 16), stage_at + j * 1024);
-    }
+      for (int j = 0; j < C::NLOAD; ++j) dma16(kt + j * 1024, off_k[j % PK], stage_at + j * 1024);
 #pragma unroll
-    for (int j = 0; j < C::NLOAD; ++j) {
-      const int c = j * 64 + lane, r = c / C::CPR, pc = c % C::CPR;
-      dma16(vt, (uint32_t)(min(r, last) * C::ROWB + ((pc - C::rot_v(r)) & (C::CPR - 1)) * 16), stage_at + C::OPB + j * 1024);
+      for (int j = 0; j < C::NLOAD; ++j) dma16(vt + j * 1024, off_v, stage_at + C::OPB + j * 1024);
+    } else {
+      // rows past the end read the last key (their scores are masked)
+#pragma unroll
+      for (int j = 0; j < C::NLOAD; ++j) {
+        const int r = ROWS1 * j + lrow, back = max(r - (nvalid - 1), 0) * C::ROWB;
+        dma16(kt, (uint32_t)(off_k[j % PK] + j * 1024 - back), stage_at + j * 1024);
+      }
+#pragma unroll
+      for (int j = 0; j < C::NLOAD; ++j) {
+        const int r = ROWS1 * j + lrow, back = max(r - (nvalid - 1), 0) * C::ROWB;
+        dma16(vt, (uint32_t)(off_v + j * 1024 - back), stage_at + C::OPB + j * 1024);
+      }
     }
     wait_vm<C::NLOAD>();                                      // the keys are there
     f32x16 s[C::NKB];
@@ -137,14 +185,19 @@ __global__ __launch_bounds__(256, 2) void shared_finish_kernel(const FinishParam
         s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qreg[ks], s[kb], 0, 0, 0);
       }
     // s[kb][r]: row lane % 32, key 32 kb + 8 (r / 4) + 4 h + r % 4
+    if (ragged) {
+      asm volatile("" ::: "memory");                          // a branch, not a select for every score
+#pragma unroll
+      for (int kb = 0; kb < C::NKB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (32 * kb + 8 * (r / 4) + 4 * h + (r % 4) >= nvalid) s[kb][r] = -INFINITY;
+    }
     float tmax = -INFINITY;
 #pragma unroll
     for (int kb = 0; kb < C::NKB; ++kb)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        if (32 * kb + 8 * (r / 4) + 4 * h + (r % 4) >= nvalid) s[kb][r] = -INFINITY;
-        tmax = fmaxf(tmax, s[kb][r]);
-      }
+      for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, s[kb][r]);
     tmax = max_halves(tmax * p.scale_log2);
     const float m_new = tmax > acc.m + 8.f ? tmax : acc.m;    // moves rarely: weights stay below 2^8
     const float m_use = m_new == -INFINITY ? 0.f : m_new;
@@ -168,7 +221,7 @@ __global__ __launch_bounds__(256, 2) void shared_finish_kernel(const FinishParam
         for (int r = 0; r < 16; ++r) acc.o[db][r] *= alpha;
     }
     wait_vm<0>();
-    if (nvalid < C::KT) {
+    if (ragged) {
       // value rows past the end: a weight of 0 must not meet an infinity or NaN of the duplicated last key
       for (int c = nvalid * C::CPR + lane; c < C::KT * C::CPR; c += 64) *(f32x4*)(stage + C::OPB + c * 16) = f32x4{0.f, 0.f, 0.f, 0.f};
       // other lanes of the wavefront read them: LDS keeps the order by itself, the compiler is told
@@ -188,22 +241,22 @@ __global__ __launch_bounds__(256, 2) void shared_finish_kernel(const FinishParam
       }
   };
 
-  FinAcc<C::NDB> ext, blk;
-  ext.init();
-  blk.init();
+  FinAcc<C::NDB> acc;
+  acc.init();
   const bool step = p.k_block != nullptr;                     // uniform
+  const int nown = step ? kWaves - 1 : kWaves;                // wavefronts for the own keys
   if (step && wave == kBlockWave) {
     const size_t off = (size_t)(b * p.Hkv + kvh) * p.Bq * C::ROWB;
-    tile(blk, (const unsigned char*)p.k_block + off, (const unsigned char*)p.v_block + off, p.Bq);
+    tile(acc, (const unsigned char*)p.k_block + off, (const unsigned char*)p.v_block + off, p.Bq);
   }
   const int ntiles = (nkeys + C::KT - 1) / C::KT;
-  for (int t = wave; t < ntiles; t += kWaves) {
+  for (int t = wave; t < ntiles && wave < nown; t += nown) {
     const int k0 = t * C::KT, slot = (int)fastdiv((uint32_t)k0, p.div_page);
     page = min(max(page, 0), p.num_pages - 1);                // clamped into the pool
     const size_t off = (((size_t)page * p.Hkv + kvh) * p.div_page.d + (k0 - slot * (int)p.div_page.d)) * C::ROWB;
-    const int k1 = min(k0 + kWaves * C::KT, nkeys - 1);       // the next tile's page, or the last one again
+    const int k1 = min(k0 + nown * C::KT, nkeys - 1);       // the next tile's page, or the last one again
     page = sload(p.block_table + (size_t)b * p.max_pages, (int)fastdiv((uint32_t)k1, p.div_page));
-    tile(ext, (const unsigned char*)p.k_pool + off, (const unsigned char*)p.v_pool + off, nkeys - k0);
+    tile(acc, (const unsigned char*)p.k_pool + off, (const unsigned char*)p.v_pool + off, nkeys - k0);
   }
 
   // ---- records of 64 columns: [wavefronts: own keys][block][groups of splits][32 rows]
@@ -233,14 +286,16 @@ __global__ __launch_bounds__(256, 2) void shared_finish_kernel(const FinishParam
   };
   // this group's split partials, of all columns in one memory round trip
   constexpr int NH = D / 64;
-  Part8 folded[NH];
+  Folded<NH> f;
+  f.m = -INFINITY;
+  f.l = 0.f;
 #pragma unroll
-  for (int half = 0; half < NH; ++half) folded[half] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}, -INFINITY, 0.f};
+  for (int half = 0; half < NH; ++half) f.a[half] = f.b[half] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (row < valid) {
-    constexpr int CH = 4;                                     // splits in a round trip
+    constexpr int CH = 12 / NH;                               // splits in a round trip
     for (int s0 = slice; s0 < p.nsplit; s0 += slices * CH) {
       f32x4 oa[CH][NH], ob[CH][NH];
-      float mv[CH], lv[CH], cm = folded[0].m;
+      float mv[CH], lv[CH], cm = f.m;
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
         const int s = s0 + c * slices;
@@ -263,74 +318,128 @@ __global__ __launch_bounds__(256, 2) void shared_finish_kernel(const FinishParam
 #pragma unroll
       for (int c = 0; c < CH; ++c) cm = fmaxf(cm, mv[c]);
       if (cm == -INFINITY) continue;
-      const float w = __builtin_amdgcn_exp2f(folded[0].m - cm);
+      const float back = __builtin_amdgcn_exp2f(f.m - cm);
+      float w[CH];
 #pragma unroll
-      for (int half = 0; half < NH; ++half) {
-        Part8& f = folded[half];
-        f.a *= w;
-        f.b *= w;
-        f.l *= w;
-        f.m = cm;
+      for (int c = 0; c < CH; ++c) w[c] = __builtin_amdgcn_exp2f(mv[c] - cm);
+      f.m = cm;
+      f.l *= back;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) add_part(f, oa[c][half], ob[c][half], lv[c], __builtin_amdgcn_exp2f(mv[c] - cm));
-      }
-    }
-  }
+      for (int c = 0; c < CH; ++c) f.l = fmaf(lv[c], w[c], f.l);
 #pragma unroll
-  for (int half = 0; half < NH; ++half) {
-    const Part8& f = folded[half];
-    __syncthreads();                                          // the stages, or the records of the first 64 columns, have been read
-    if (ntiles > 0) put(ext, wave, half);
-    if (step && wave == kBlockWave) put(blk, kWaves, half);
-    *(f32x4*)(rec + ((kWaves + 1) * 32 + group) * C::RS + 8 * part) = f.a;
-    *(f32x4*)(rec + ((kWaves + 1) * 32 + group) * C::RS + 8 * part + 4) = f.b;
-    if (part == 0) stat[(kWaves + 1) * 32 + group] = make_float2(f.m, f.l);
-    __syncthreads();
-    if (group < valid) {                                      // (slice 0: group is the row)
-      const size_t g = grow0 + group;
-      const int nw = ntiles > 0 ? kWaves : 0, col = 64 * half + 8 * part;
-      float M = -INFINITY;
-      for (int w = 0; w < nw; ++w) M = fmaxf(M, stat[w * 32 + group].x);
-      for (int s = 0; s < slices; ++s) M = fmaxf(M, stat[(kWaves + 1) * 32 + s * rv + group].x);
-      const float Mu = M == -INFINITY ? 0.f : M;
-      Part8 t = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}, M, 0.f};
-      auto add = [&](int at) {
-        const float2 ml = stat[at];
-        const float* o = rec + at * C::RS + 8 * part;
-        add_part(t, *(const f32x4*)o, *(const f32x4*)(o + 4), ml.y, __builtin_amdgcn_exp2f(ml.x - Mu));
-      };
-      for (int s = 0; s < slices; ++s) add((kWaves + 1) * 32 + s * rv + group);
-      for (int w = 0; w < nw; ++w) add(w * 32 + group);
-      // the partial, in natural-log units: m is rounded when converted, o is rescaled to the reference that consumers recover from it
-      float m_nat = -INFINITY, L = -INFINITY, adj = 0.f;
-      if (t.l > 0.f) {
-        m_nat = M * kLn2;
-        adj = __builtin_amdgcn_exp2f(M - m_nat * kLog2e);
-        L = (M + log2f(t.l)) * kLn2;
-      }
-      *(f32x4*)(p.o + g * D + col) = t.a * adj;
-      *(f32x4*)(p.o + g * D + col + 4) = t.b * adj;
-      if (part == 0 && half == 0) {
-        p.m[g] = m_nat;
-        p.lse[g] = L;
-      }
-      if (step) {
-        const float2 ml = stat[kWaves * 32 + group];
-        const float* o = rec + (kWaves * 32 + group) * C::RS + 8 * part;
-        const f32x4 ia = *(const f32x4*)o, ib = *(const f32x4*)(o + 4);
-        const float M2 = fmaxf(M, ml.x), M2u = M2 == -INFINITY ? 0.f : M2;
-        const float we = __builtin_amdgcn_exp2f(M - M2u), wi = __builtin_amdgcn_exp2f(ml.x - M2u);
-        const float den = t.l * we + ml.y * wi;
-        const float inv = den > 0.f ? 1.f / den : 0.f;
-        float r[8];
+      for (int half = 0; half < NH; ++half)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          r[i] = (t.a[i] * we + ia[i] * wi) * inv;
-          r[4 + i] = (t.b[i] * we + ib[i] * wi) * inv;
+          f.a[half][i] *= back;
+          f.b[half][i] *= back;
+#pragma unroll
+          for (int c = 0; c < CH; ++c) {
+            f.a[half][i] = fmaf(oa[c][half][i], w[c], f.a[half][i]);
+            f.b[half][i] = fmaf(ob[c][half][i], w[c], f.b[half][i]);
+          }
+        }
+    }
+  }
+  // groups of a wavefront that have the same row: lanes 32, 16, 8 across; what is left goes through LDS, at most kWaves to a row
+  if (rv_log2 <= 2) fold_lanes<NH, kAcross32>(f);
+  if (rv_log2 <= 1) fold_lanes<NH, kAcross16>(f);
+  if (rv_log2 == 0) fold_lanes<NH, kAcross8>(f);
+  const int inside = max(0, 3 - rv_log2), nslots = slices >> inside, slot = slice >> inside;
+  const bool writes = (slice & ((1 << inside) - 1)) == 0;
+  const int nw = ntiles > 0 ? nown : 0;
+  // a thread of the end: row `group`, 8 columns of each 64; weights of the slots and of the wavefronts
+  float ws[kWaves], ww[kWaves], wblk = 0.f, wext = 0.f, M = -INFINITY, adj = 0.f;
+#pragma unroll
+  for (int half = 0; half < NH; ++half) {
+    __syncthreads();                                          // the stages, or the records of the first 64 columns, have been read
+    put(acc, wave, half);
+    if (writes) {
+      const int at = kWaves * 32 + slot * rv + row;
+      *(f32x4*)(rec + at * C::RS + 8 * part) = f.a[half];
+      *(f32x4*)(rec + at * C::RS + 8 * part + 4) = f.b[half];
+      if (part == 0 && half == 0) stat[at] = make_float2(f.m, f.l);
+    }
+    __syncthreads();
+    if (group < valid) {
+      const size_t g = grow0 + group;
+      const int col = 64 * half + 8 * part;
+      // (what is not there is read in the place of the first one and left out below: reads in front of the branches overlap)
+      auto slot_at = [&](int i) { return kWaves * 32 + (i < nslots ? i : 0) * rv + group; };
+      auto wave_at = [&](int i) { return (i < nw ? i : 0) * 32 + group; };
+      if (half == 0) {
+        float2 ss[kWaves], sw[kWaves];
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+          ss[i] = stat[slot_at(i)];
+          sw[i] = stat[wave_at(i)];
+        }
+        const float2 sb = stat[kBlockWave * 32 + group];
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+          if (i < nslots) M = fmaxf(M, ss[i].x);
+          if (i < nw) M = fmaxf(M, sw[i].x);
+        }
+        const float Mu = M == -INFINITY ? 0.f : M;
+        float l = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+          ws[i] = __builtin_amdgcn_exp2f(ss[i].x - Mu);
+          if (i < nslots) l = fmaf(ss[i].y, ws[i], l);
+        }
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+          ww[i] = __builtin_amdgcn_exp2f(sw[i].x - Mu);
+          if (i < nw) l = fmaf(sw[i].y, ww[i], l);
+        }
+        // the partial, in natural-log units: m is rounded when converted, o is rescaled to the reference that consumers recover from it
+        float m_nat = -INFINITY, L = -INFINITY;
+        if (l > 0.f) {
+          m_nat = M * kLn2;
+          adj = __builtin_amdgcn_exp2f(M - m_nat * kLog2e);
+          L = (M + log2f(l)) * kLn2;
+        }
+        if (part == 0) {
+          p.m[g] = m_nat;
+          p.lse[g] = L;
+        }
+        if (step) {
+          const float M2 = fmaxf(M, sb.x), M2u = M2 == -INFINITY ? 0.f : M2;
+          wext = __builtin_amdgcn_exp2f(M - M2u);
+          wblk = __builtin_amdgcn_exp2f(sb.x - M2u);
+          const float den = l * wext + sb.y * wblk, inv = den > 0.f ? 1.f / den : 0.f;
+          wext *= inv;
+          wblk *= inv;
+          if (part == 0 && p.lse_out != nullptr) p.lse_out[g] = den > 0.f ? (M2 + log2f(den)) * kLn2 : -INFINITY;
+        }
+      }
+      f32x4 va[2 * kWaves + 1], vb[2 * kWaves + 1], ta = {0.f, 0.f, 0.f, 0.f}, tb = ta;
+#pragma unroll
+      for (int i = 0; i <= 2 * kWaves; ++i) {
+        const float* o = rec + (i < kWaves ? slot_at(i) : i < 2 * kWaves ? wave_at(i - kWaves) : kBlockWave * 32 + group) * C::RS + 8 * part;
+        va[i] = *(const f32x4*)o;
+        vb[i] = *(const f32x4*)(o + 4);
+      }
+#pragma unroll
+      for (int i = 0; i < 2 * kWaves; ++i)
+        if (i < kWaves ? i < nslots : i - kWaves < nw) {
+          const float w = i < kWaves ? ws[i % kWaves] : ww[i % kWaves];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            ta[j] = fmaf(va[i][j], w, ta[j]);
+            tb[j] = fmaf(vb[i][j], w, tb[j]);
+          }
+        }
+      *(f32x4*)(p.o + g * D + col) = ta * adj;
+      *(f32x4*)(p.o + g * D + col + 4) = tb * adj;
+      if (step) {
+        float r[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          r[j] = ta[j] * wext + va[2 * kWaves][j] * wblk;
+          r[4 + j] = tb[j] * wext + vb[2 * kWaves][j] * wblk;
         }
         const u32x4 pk = {pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3]), pack_bf16x2(r[4], r[5]), pack_bf16x2(r[6], r[7])};
         *(u32x4*)((__bf16*)p.out + g * D + col) = pk;
-        if (part == 0 && half == 0 && p.lse_out != nullptr) p.lse_out[g] = den > 0.f ? (M2 + log2f(den)) * kLn2 : -INFINITY;
       }
     }
   }
