@@ -1357,6 +1357,8 @@ fb_status shared_partials(const fb_shape* shape, const void* q, const fb_paged_k
   int32_t* order = by_length ? (int32_t*)(ws + w.order) : nullptr;
   if (shape->dtype == FB_BF16 && plan.ns_shared > 0) {
     e = fb::launch_shared_bf16(sh, p, order, plan.rows, shape->head_dim, stream);
+  } else if (shape->dtype == FB_F32 && plan.ns_shared > 0 && own) {
+    e = fb::launch_shared_f32(sh, p, shape->head_dim, stream);
   } else {
     if (plan.ns_shared > 0) e = launch_attn(shape, sh, fb::kPassShared, stream);
     if (e == hipSuccess && own) e = launch_attn(shape, p, fb::kPassDensePaged, stream);

@@ -293,9 +293,9 @@ __device__ __forceinline__ void f32_tile(FState<RB, D / 16>& st, const f32x4 (&q
 // Products of a pass: fp32; of bf16 parts; fp32 again, half of the rows at a time, where those of parts gave a NaN.
 enum F32Products : int { kProductsF32, kProductsParts, kProductsAgain };
 
-// The pass of one workgroup.  kProductsParts: false, and nothing stored, where a NaN came out.  half: of the rows, kProductsAgain.
+// The pass of one workgroup, wg_at of nwgs.  kProductsParts: false, and nothing stored, where a NaN came out.  half: of the rows, kProductsAgain.
 template <int D, int MODE, int RB, int WR, int TG, int PRODUCTS>
-__device__ __forceinline__ bool f32_pass(const PassParams& p, unsigned char* ring, int half = 0) {
+__device__ __forceinline__ bool f32_pass(const PassParams& p, unsigned char* ring, uint32_t wg_at, uint32_t nwgs, int half = 0) {
   constexpr bool PARTS = PRODUCTS == kProductsParts;
   using C = FCfg<D, RB, WR, TG>;
   constexpr bool kPerHead = f32_per_head(MODE);
@@ -309,7 +309,7 @@ __device__ __forceinline__ bool f32_pass(const PassParams& p, unsigned char* rin
     x = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
     asm volatile("" : "+v"(x));
   };
-  int lane = threadIdx.x & 63, wg = blockIdx.x;
+  int lane = threadIdx.x & 63, wg = wg_at;
   if constexpr (PRODUCTS == kProductsAgain) {
     lane_again(lane);
     asm volatile("" : "+s"(wg));
@@ -330,7 +330,7 @@ __device__ __forceinline__ bool f32_pass(const PassParams& p, unsigned char* rin
     rest = jq * 8 + xcd;
     if (rest >= (uint32_t)(p.B * p.Hkv * p.nsplit)) return true;   // workgroup-uniform
   } else {
-    const int bid = wg, q8 = gridDim.x / 8, r8 = gridDim.x % 8, xcd = bid % 8;
+    const int bid = wg, q8 = nwgs / 8, r8 = nwgs % 8, xcd = bid % 8;
     const int w = (xcd < r8 ? xcd * (q8 + 1) : r8 * (q8 + 1) + (xcd - r8) * q8) + bid / 8;
     rest = fastdiv((uint32_t)w, p.div_rowtiles);
     rt = w - (int)(rest * p.div_rowtiles.d);
@@ -681,23 +681,42 @@ __device__ __forceinline__ bool f32_pass(const PassParams& p, unsigned char* rin
 // 64-row workgroups: an infinity has no parts (its remainder is NaN), a part of 0 must not meet one, and parts of opposite signs may
 // overflow where their sum does not.  All of it leaves a NaN in the row sums or the accumulators of the pass by parts; such a
 // workgroup does its pass over again with the fp32 products, so that a value counts for what it does in the other workgroups.
-template <int D, int MODE, int RB, int WR, int TG = 1, bool PARTS = FCfg<D, RB, WR, TG>::kParts>
-__global__ __launch_bounds__(256 * WR * TG, 1) void attn_f32_kernel(const PassParams p) {
-  extern __shared__ __align__(16) unsigned char ring[];
+// p_at: byte of the kernel's arguments that p is at.
+template <int D, int MODE, int RB, int WR, int TG, bool PARTS>
+__device__ __forceinline__ void f32_workgroup(const PassParams& p, uint32_t p_at, unsigned char* ring, uint32_t wg, uint32_t nwgs) {
   if constexpr (PARTS) {
-    if (f32_pass<D, MODE, RB, WR, TG, kProductsParts>(p, ring)) return;
-    // (p is the only argument: read again from where the arguments are, instead of kept in registers throughout the first pass)
-    typedef const __attribute__((address_space(4))) PassParams* Args;
-    Args args = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+    if (f32_pass<D, MODE, RB, WR, TG, kProductsParts>(p, ring, wg, nwgs)) return;
+    // (read again from where the arguments are, instead of kept in registers throughout the first pass)
+    typedef const __attribute__((address_space(4))) char* Args;
+    Args args = (Args)__builtin_amdgcn_kernarg_segment_ptr() + p_at;
     asm volatile("" : "+s"(args));
 #pragma unroll 1
     for (int half = 0; half < 2; ++half) {
       __syncthreads();                                          // the flags, and the first half's records, have been read
-      f32_pass<D, MODE, RB / 2, WR, TG, kProductsAgain>(*(const PassParams*)args, ring, half);
+      f32_pass<D, MODE, RB / 2, WR, TG, kProductsAgain>(*(const PassParams*)(const __attribute__((address_space(4))) PassParams*)args, ring, wg, nwgs, half);
     }
   } else {
-    f32_pass<D, MODE, RB, WR, TG, kProductsF32>(p, ring);
+    f32_pass<D, MODE, RB, WR, TG, kProductsF32>(p, ring, wg, nwgs);
   }
+}
+
+template <int D, int MODE, int RB, int WR, int TG = 1, bool PARTS = FCfg<D, RB, WR, TG>::kParts>
+__global__ __launch_bounds__(256 * WR * TG, 1) void attn_f32_kernel(const PassParams p) {
+  extern __shared__ __align__(16) unsigned char ring[];
+  f32_workgroup<D, MODE, RB, WR, TG, PARTS>(p, 0, ring, blockIdx.x, gridDim.x);
+}
+
+// Shared prefix: the pass over the shared keys and the paged pass over the sequences' own keys, where both take workgroups of the same
+// kind, in one launch.
+struct SharedF32Params {
+  PassParams shared, own;
+  uint32_t shared_wgs;
+};
+template <int D, int RB, int WR, bool PARTS>
+__global__ __launch_bounds__(256 * WR, 1) void attn_shared_f32_kernel(const SharedF32Params p) {
+  extern __shared__ __align__(16) unsigned char ring[];
+  if (blockIdx.x < p.shared_wgs) f32_workgroup<D, kPassShared, RB, WR, 1, PARTS>(p.shared, 0, ring, blockIdx.x, p.shared_wgs);
+  else f32_workgroup<D, kPassDensePaged, RB, WR, 1, PARTS>(p.own, offsetof(SharedF32Params, own), ring, blockIdx.x - p.shared_wgs, gridDim.x - p.shared_wgs);
 }
 
 // Attention mass per (query row, key block): sum over the block's keys of exp(s - lse), fp32 storage.
@@ -994,6 +1013,26 @@ inline int few_tiles_f32(long long workgroups, bool internal) {
   return workgroups > 768 ? 8 : workgroups > 512 ? 4 : 3;
 }
 
+// The parameters a pass is launched with, in q; its workgroups, 0: too many.
+template <int D, int MODE, int RB, int WR, int TG>
+unsigned f32_grid(const PassParams& p, PassParams& q) {
+  using C = FCfg<D, RB, WR, TG>;
+  constexpr bool per_head = f32_per_head(MODE);
+  const int heads = per_head ? p.Hq : p.Hkv, nrows = per_head ? p.Bq : p.G * p.Bq;
+  const int rowtiles = (nrows + C::ROWS - 1) / C::ROWS;
+  const int nsplit = p.nsplit + (MODE == kPassRefreshFused ? 1 : 0);
+  long long units = (long long)p.B * heads * nsplit;
+  if (MODE == kPassDensePaged) units = (units + 7) / 8 * 8;
+  if (units * rowtiles >= (1ll << 31)) return 0;
+  q = p;
+  if (MODE == kPassDensePaged || MODE == kPassShared) q.div_page = make_fastdiv((uint32_t)p.page_size);
+  if (MODE == kPassShared) q.div_tpb = make_fastdiv((uint32_t)p.key_block);
+  q.div_rowtiles = make_fastdiv((uint32_t)rowtiles);
+  q.div_nsplit = make_fastdiv((uint32_t)nsplit);
+  q.div_hkv = make_fastdiv((uint32_t)heads);
+  return (unsigned)(units * rowtiles);
+}
+
 template <int D, int MODE, int RB, int WR, int TG = 1, bool PARTS = FCfg<D, RB, WR, TG>::kParts>
 hipError_t launch_f32(const PassParams& p, hipStream_t s) {
   using C = FCfg<D, RB, WR, TG>;
@@ -1001,21 +1040,62 @@ hipError_t launch_f32(const PassParams& p, hipStream_t s) {
   static LdsLimit lim;
   hipError_t e = raise_lds_limit(kern, C::LDS, lim, C::LDS);
   if (e != hipSuccess) return e;
-  constexpr bool per_head = f32_per_head(MODE);
-  const int heads = per_head ? p.Hq : p.Hkv, nrows = per_head ? p.Bq : p.G * p.Bq;
-  const int rowtiles = (nrows + C::ROWS - 1) / C::ROWS;
-  const int nsplit = p.nsplit + (MODE == kPassRefreshFused ? 1 : 0);
-  long long units = (long long)p.B * heads * nsplit;
-  if (MODE == kPassDensePaged) units = (units + 7) / 8 * 8;
-  if (units * rowtiles >= (1ll << 31)) return hipErrorInvalidValue;
-  PassParams q = p;
-  if (MODE == kPassDensePaged || MODE == kPassShared) q.div_page = make_fastdiv((uint32_t)p.page_size);
-  if (MODE == kPassShared) q.div_tpb = make_fastdiv((uint32_t)p.key_block);
-  q.div_rowtiles = make_fastdiv((uint32_t)rowtiles);
-  q.div_nsplit = make_fastdiv((uint32_t)nsplit);
-  q.div_hkv = make_fastdiv((uint32_t)heads);
-  hipLaunchKernelGGL(kern, dim3((unsigned)(units * rowtiles)), dim3(C::THREADS), C::LDS, s, q);
+  PassParams q;
+  const unsigned grid = f32_grid<D, MODE, RB, WR, TG>(p, q);
+  if (grid == 0) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(kern, dim3(grid), dim3(C::THREADS), C::LDS, s, q);
   return hipGetLastError();
+}
+
+// Workgroups of a pass: 16, 32 or 64 rows; 64 with products from bf16 parts.
+enum F32Kind : int { kF32Rows16, kF32Rows32, kF32Rows64, kF32Rows64Parts };
+
+template <int D, int RB, int WR, bool PARTS>
+hipError_t launch_shared_f32_kind(const PassParams& shared, const PassParams& own, hipStream_t s) {
+  using C = FCfg<D, RB, WR>;
+  auto kern = attn_shared_f32_kernel<D, RB, WR, PARTS>;
+  static LdsLimit lim;
+  hipError_t e = raise_lds_limit(kern, C::LDS, lim, C::LDS);
+  if (e != hipSuccess) return e;
+  SharedF32Params q;
+  const unsigned nshared = f32_grid<D, kPassShared, RB, WR, 1>(shared, q.shared), nown = f32_grid<D, kPassDensePaged, RB, WR, 1>(own, q.own);
+  if (nshared == 0 || nown == 0 || (long long)nshared + nown >= (1ll << 31)) return hipErrorInvalidValue;
+  q.shared_wgs = nshared;
+  hipLaunchKernelGGL(kern, dim3(nshared + nown), dim3(C::THREADS), C::LDS, s, q);
+  return hipGetLastError();
+}
+
+// The workgroups of a pass, by its rows, splits and tiles.
+template <int D, int MODE>
+F32Kind f32_kind(const PassParams& p) {
+  const int nrows = f32_per_head(MODE) ? p.Bq : p.G * p.Bq;
+  int tile = f32_row_tile(nrows);
+  if (MODE == kPassInternal) {
+    // the internal pass has no splits to fill the chip with: 16-row workgroups until 64-row ones do (blocks of 32, 64-row
+    // workgroups: 16 of them 14.2 us, 7.2 with 16 rows; 128 14.8 and 13.2; 256 15.5 and 23.8; blocks of 1000, 192 of them, 85
+    // and 105)
+    if ((long long)p.B * p.Hkv * ((nrows + 63) / 64) < 256) tile = 16;
+  } else {
+    // too few tiles for the splits that would fill the chip: smaller workgroups as long as they are one round (128 rows of 8
+    // KV heads, head_dim 128, 32 / 64 / 192 keys: 64-row workgroups 12.9 / 12.7 / 15.5 us, 16-row ones 6.4 / 6.2 / 9.2)
+    const long long units = (long long)p.B * (f32_per_head(MODE) ? p.Hq : p.Hkv) * (p.nsplit + (MODE == kPassRefreshFused ? 1 : 0));
+    if (units * ((nrows + 15) / 16) <= 256) tile = 16;
+    else if (tile > 32 && units * ((nrows + 31) / 32) <= 256) tile = 32;
+  }
+  if (tile == 16) return kF32Rows16;
+  // two accumulator sets at head_dim 128: 64-row workgroups have half the registers a wavefront and spill in the tile loop
+  // (32 / 8 heads of 40 rows, 4111 keys, refresh 138 us with 64 rows and 82 with 32)
+  constexpr bool fits64 = !(D == 128 && MODE == kPassSparseRefresh);
+  if constexpr (fits64) {
+    // (sparse reuse: how many tiles a head has is not known here, and it always takes the parts)
+    if constexpr (D == 64 && MODE != kPassSparseReuse) {
+      const int splits = MODE == kPassInternal ? 1 : p.nsplit;
+      const long long workgroups = (long long)p.B * (f32_per_head(MODE) ? p.Hq : p.Hkv) * splits * ((nrows + 63) / 64);
+      if (tile > 32 && (p.nkeys + kKeyTile - 1) / kKeyTile <= few_tiles_f32(workgroups, MODE == kPassInternal) * splits) return kF32Rows64;
+    }
+    if (tile > 32) return kF32Rows64Parts;
+  }
+  return kF32Rows32;
 }
 
 template <int D, int MODE>
@@ -1034,33 +1114,17 @@ hipError_t launch_f32_rows(const PassParams& p, hipStream_t s) {
     const long long most = p.nkeys <= 32 ? 2048 : p.nkeys <= 48 ? (D == 64 ? 1536 : 512) : 256;
     if (p.nkeys > kFewKeysF32 && p.nkeys <= 64 && waves <= most && !internal_in_place(p, D, 4)) return launch_internal_f32_wave<D>(p, s);
   }
-  int tile = f32_row_tile(nrows);
-  if (MODE == kPassInternal) {
-    // the internal pass has no splits to fill the chip with: 16-row workgroups until 64-row ones do (blocks of 32, 64-row
-    // workgroups: 16 of them 14.2 us, 7.2 with 16 rows; 128 14.8 and 13.2; 256 15.5 and 23.8; blocks of 1000, 192 of them, 85
-    // and 105)
-    if ((long long)p.B * p.Hkv * ((nrows + 63) / 64) < 256) tile = 16;
-  } else {
-    // too few tiles for the splits that would fill the chip: smaller workgroups as long as they are one round (128 rows of 8
-    // KV heads, head_dim 128, 32 / 64 / 192 keys: 64-row workgroups 12.9 / 12.7 / 15.5 us, 16-row ones 6.4 / 6.2 / 9.2)
-    const long long units = (long long)p.B * (f32_per_head(MODE) ? p.Hq : p.Hkv) * (p.nsplit + (MODE == kPassRefreshFused ? 1 : 0));
-    if (units * ((nrows + 15) / 16) <= 256) tile = 16;
-    else if (tile > 32 && units * ((nrows + 31) / 32) <= 256) tile = 32;
+  switch (f32_kind<D, MODE>(p)) {
+    case kF32Rows16: return launch_f32<D, MODE, 1, 1>(p, s);
+    case kF32Rows32: return launch_f32<D, MODE, 2, 1>(p, s);
+    case kF32Rows64:
+      if constexpr (D == 64 && MODE != kPassSparseReuse) return launch_f32<D, MODE, 2, 2, 1, false>(p, s);
+      break;
+    case kF32Rows64Parts:
+      if constexpr (!(D == 128 && MODE == kPassSparseRefresh)) return launch_f32<D, MODE, 2, 2>(p, s);
+      break;
   }
-  if (tile == 16) return launch_f32<D, MODE, 1, 1>(p, s);
-  // two accumulator sets at head_dim 128: 64-row workgroups have half the registers a wavefront and spill in the tile loop
-  // (32 / 8 heads of 40 rows, 4111 keys, refresh 138 us with 64 rows and 82 with 32)
-  constexpr bool fits64 = !(D == 128 && MODE == kPassSparseRefresh);
-  if constexpr (fits64) {
-    // (sparse reuse: how many tiles a head has is not known here, and it always takes the parts)
-    if constexpr (D == 64 && MODE != kPassSparseReuse) {
-      const int splits = MODE == kPassInternal ? 1 : p.nsplit;
-      const long long workgroups = (long long)p.B * (f32_per_head(MODE) ? p.Hq : p.Hkv) * splits * ((nrows + 63) / 64);
-      if (tile > 32 && (p.nkeys + kKeyTile - 1) / kKeyTile <= few_tiles_f32(workgroups, MODE == kPassInternal) * splits) return launch_f32<D, MODE, 2, 2, 1, false>(p, s);
-    }
-    if (tile > 32) return launch_f32<D, MODE, 2, 2>(p, s);
-  }
-  return launch_f32<D, MODE, 2, 1>(p, s);
+  return hipErrorInvalidValue;
 }
 
 template <int D>
@@ -1086,6 +1150,28 @@ hipError_t launch_block_mass_f32(const MassParams& p, int D, hipStream_t s) {
   if (D == 64) hipLaunchKernelGGL(block_mass_f32_kernel<64>, grid, dim3(256), 0, s, p);
   else hipLaunchKernelGGL(block_mass_f32_kernel<128>, grid, dim3(256), 0, s, p);
   return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_shared_f32_d(const PassParams& shared, const PassParams& own, hipStream_t s) {
+  const F32Kind kind = f32_kind<D, kPassShared>(shared);
+  if (kind != f32_kind<D, kPassDensePaged>(own)) {
+    const hipError_t e = launch_d<D>(shared, kPassShared, s);
+    return e == hipSuccess ? launch_d<D>(own, kPassDensePaged, s) : e;
+  }
+  switch (kind) {
+    case kF32Rows16: return launch_shared_f32_kind<D, 1, 1, false>(shared, own, s);
+    case kF32Rows32: return launch_shared_f32_kind<D, 2, 1, false>(shared, own, s);
+    case kF32Rows64:
+      if constexpr (D == 64) return launch_shared_f32_kind<D, 2, 2, false>(shared, own, s);
+      break;
+    case kF32Rows64Parts: return launch_shared_f32_kind<D, 2, 2, true>(shared, own, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_shared_f32(const PassParams& shared, const PassParams& own, int D, hipStream_t s) {
+  return D == 64 ? launch_shared_f32_d<64>(shared, own, s) : launch_shared_f32_d<128>(shared, own, s);
 }
 
 hipError_t launch_attn_f32(const PassParams& p, int D, PassMode mode, hipStream_t s) {

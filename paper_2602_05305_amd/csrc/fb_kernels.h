@@ -261,6 +261,8 @@ int stream_bf16_name(const PassParams& p, int D, PassMode mode, char* buf, size_
 // Rows of a workgroup (256: of 8 wavefronts of 32 rows, or of 4 of 64, which needs kRowsTiles tiles to a split).
 enum SharedRows : int { kShared32, kShared64, kShared128, kShared256Short, kShared256 };
 hipError_t launch_shared_bf16(const PassParams& shared, const PassParams& own, int32_t* order, SharedRows rows, int D, hipStream_t s);
+// Both passes, fp32: in one launch where their workgroups are of one kind, else one after the other.
+hipError_t launch_shared_f32(const PassParams& shared, const PassParams& own, int D, hipStream_t s);
 // Whether the internal pass of p can fold p.fold_ns split partials itself (few splits; not the row-pair kernels).
 bool internal_fold_covers(const PassParams& p, int D);
 // Name of the kernel launch_attn_bf16 runs for the dense external pass of p (profiler spelling, no namespace).
