@@ -117,6 +117,18 @@ __device__ __forceinline__ void dma16_at(const void* base, uint32_t off, uint32_
                : "memory", "m0", "scc");
 }
 
+// Value rows [from, to) of a tile in LDS, past the end of the keys, become 0: a weight of 0 must not meet an infinity of the duplicated last
+// key.  Every wavefront that reads them clears them itself, before it does; another one's zeros change nothing.
+template <int D>
+__device__ __forceinline__ void clear_rows(unsigned char* rows, int from, int to, int lane) {
+  constexpr int CPR = D * 2 / 16;
+  for (int c = from * CPR + lane; c < to * CPR; c += 64) *(f32x4*)(rows + c * 16) = f32x4{0.f, 0.f, 0.f, 0.f};
+  // other lanes of the wavefront read them: LDS keeps the order by itself, the compiler is told (no instruction)
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 template <int D, int MODE>
 __device__ __forceinline__ void rows_pass(const PassParams& p, unsigned char* ring, uint32_t wg, uint32_t nwgs) {
   using C = RCfg<D>;
@@ -484,6 +496,7 @@ __device__ __forceinline__ void rows_pass(const PassParams& p, unsigned char* ri
     if (moved || (unsigned)(t - t_ragged + 5) <= 5u || t + 5 >= again) {
       // rare: the reference moved, or the ragged tile is near: requested in this iteration or the last one, or computed now
       if (t == t_ragged) {
+        if constexpr (kShared) clear_rows<D>(ring + VOFF + tt % C::NS * C::OPB, nvalid, C::KT, lane);      // (its operands are read below)
         mask_tile(s);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {

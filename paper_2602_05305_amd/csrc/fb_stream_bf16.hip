@@ -382,7 +382,7 @@ constexpr uint32_t kSegFirst = 1u, kSegReference = 2u, kSegPad = 4u;
 
 // Every layout but kRowPair: two wavefronts per row group, or one (kRowPairShort).  PARTS: the stream of a (batch element, KV head) is
 // p.nseg reference segments, each visited in an order of its own, and the workgroups take p.nsplit even pieces of that walk.
-// wg, nwgs: this workgroup of those of the pass.  ORDER: the paged pass may rank the sequences by length.
+// wg, nwgs: this workgroup of those of the pass.  ORDER: the paged pass may rank the sequences by length (not in one grid with the shared keys').
 template <int D, int MODE, int LAYOUT, int NRG, bool PARTS, bool ORDER = true>
 __device__ __forceinline__ void halves_pass(const PassParams& p, unsigned char* ring, uint32_t wg, uint32_t nwgs) {
   static_assert(!PARTS || (MODE == kPassDense && (LAYOUT == kKeySplit || LAYOUT == kTileSplit)), "reference segments: dense pass");
@@ -790,6 +790,11 @@ __device__ __forceinline__ void halves_pass(const PassParams& p, unsigned char* 
       qmask[i] = qmask[i + NNEXT];
     }
   };
+  // shared prefix: value rows past the end are cleared, where this wavefront reads them
+  constexpr bool kClear = MODE == kPassShared || (MODE == kPassDensePaged && !ORDER);
+  auto clear_ragged = [&](const unsigned char* stage, int nvalid) __attribute__((always_inline)) {
+    if (kClear && nvalid < C::KT) clear_rows<D>((unsigned char*)stage + C::OPB, max(nvalid, 32 * kb0), 32 * (kb0 + C::NKB), lane);
+  };
   // one tile of a wavefront whose row group is shared by two (key halves)
   bool seg_waits = false;          // PARTS: the segment's first tile has no key for this half (the ragged last tile): the next one counts
   auto half_tile = [&](const unsigned char* stage, int k0, uint32_t mask) __attribute__((always_inline)) {
@@ -802,6 +807,7 @@ __device__ __forceinline__ void halves_pass(const PassParams& p, unsigned char* 
     if constexpr (MODE == kPassSparseReuse) {
       if (nvalid <= 0) return;                               // a list entry past the end of the keys
     }
+    if constexpr (kClear) clear_ragged(stage, nvalid);
     bool on[NSETS];
     bool any_on = false;
 #pragma unroll
@@ -860,6 +866,10 @@ __device__ __forceinline__ void halves_pass(const PassParams& p, unsigned char* 
       if (need_b) half_tile(stage_b, k0b, mask_b);
       return;
     }
+    if constexpr (kClear) {
+      clear_ragged(stage_a, nva);
+      clear_ragged(stage_b, nvb);
+    }
     f32x16 s[2];
     two_scores<D>(s, qreg, stage_a, stage_b, kaddr, kb0);
 #pragma unroll
@@ -885,6 +895,7 @@ __device__ __forceinline__ void halves_pass(const PassParams& p, unsigned char* 
       for (int u = 0; u < 2; ++u)
         if (t + u < ntiles) {
           const unsigned char* stage = ring + ((t + u) % C::NS) * C::STAGE;
+          if constexpr (kClear) clear_ragged(stage, nkeys - qk0[u]);
           f32x16 s[C::NKB];
           tile_scores<D, C::NKB>(s, qreg, stage, kaddr, kb0);
           tile_softmax_pv<D, C::NKB>(acc, s, stage, vaddr, kb0, p.scale_log2, true, min(C::KT, nkeys - qk0[u]), h);
