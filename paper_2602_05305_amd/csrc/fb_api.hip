@@ -1284,12 +1284,38 @@ void plan_bf16(const fb_shape* s, int tiles, SharedPlan& plan) {
   plan.own_in_finish = s->prefix_len > 0 && plan.ns_own == 0;
 }
 
+// fp32: splits of the shared keys' pass, by the rows of a workgroup, which are the most that leave one round (f32_kind).  The least time by
+//   rounds of 256 workgroups * (tiles of a split * c + e), or the keys at 5.2 TB/s (head_dim 64: 7.3, small caches) if that takes longer,
+//   + 0.31 us (0.39) for every MB of split partials;
+// fitted to 2564 random calls as the bf16 one (off by 2.5 % at the median): 0.3 % longer than the best that was measured on average, 6 % in 99 of
+// 100; one round of workgroups as large as the rows allow 3.2 and 27 % (21 sequences of 8 rows of 8 KV heads, head_dim 128, 353 keys: 6 splits of 64
+// rows 23.8 us, 2 of 16 rows 17.4; 69 of 16 rows of 8 KV heads, 3948 keys: 1 split 234, 7 177).
+void plan_f32(const fb_shape* s, int tiles, SharedPlan& plan) {
+  static const struct { int rows; double c, e; } kinds[2][3] = {{{16, 1.09, -1.1}, {32, 1.71, -0.65}, {64, 2.07, 0.7}}, {{16, 1.91, 0.1}, {32, 3.15, 1.2}, {64, 3.47, 4.0}}};
+  const bool wide = s->head_dim == 128;
+  const long long nrows = rows_of(s) / s->n_kv_heads;
+  const double keys = (double)tiles * fb::kKeyTile * s->n_kv_heads * s->head_dim * 8 / (wide ? 5.2e6 : 7.3e6);
+  const double fold = (double)rows_of(s) * s->head_dim * 8e-6 * (wide ? 0.31 : 0.39);
+  const auto groups = [&](long long rows) { return s->n_kv_heads * ((nrows + rows - 1) / rows); };
+  const int most = fb::f32_row_tile(nrows) == 16 ? 0 : fb::f32_row_tile(nrows) == 32 ? 1 : 2;
+  double best = -1;
+  for (const auto& sizes : kinds[wide]) {
+    const long long g = groups(sizes.rows), tries[] = {128 / g, 256 / g, 512 / g, tiles, tiles / 2, tiles / 4, tiles / 8};
+    for (long long ns : tries) {
+      ns = std::max(1ll, std::min({ns, (long long)tiles, (long long)FB_MAX_SPLITS / 2}));
+      const int k = groups(16) * ns <= 256 ? 0 : groups(32) * ns <= 256 ? std::min(most, 1) : most;
+      const double rounds = (double)((groups(kinds[wide][k].rows) * ns + 255) / 256);
+      const double cost = std::max(rounds * ((double)((tiles + ns - 1) / ns) * kinds[wide][k].c + kinds[wide][k].e), keys) + fold * (double)ns;
+      if (best < 0 || cost < best) { best = cost; plan.ns_shared = (int)ns; }
+    }
+  }
+}
+
 SharedPlan shared_plan(const fb_shape* s, int shared_len) {
   SharedPlan plan = {0, 0, fb::kShared128, false};
   const int tiles = (shared_len + fb::kKeyTile - 1) / fb::kKeyTile;
   if (s->dtype != FB_BF16) {
-    const long long nrows = rows_of(s) / s->n_kv_heads, rt = fb::f32_row_tile(nrows), groups = s->n_kv_heads * ((nrows + rt - 1) / rt);
-    if (tiles > 0) plan.ns_shared = (int)std::max(1ll, std::min({256 / groups, (long long)tiles, (long long)FB_MAX_SPLITS / 2}));
+    if (tiles > 0) plan_f32(s, tiles, plan);
     if (s->prefix_len > 0) plan.ns_own = std::min(paged_splits(s), FB_MAX_SPLITS / 2);
     return plan;
   }
@@ -1340,9 +1366,9 @@ fb_status shared_partials(const fb_shape* shape, const void* q, const fb_paged_k
   p.page_size = kv->page_size; p.max_pages = kv->max_pages; p.num_pages = kv->num_pages;
   hipError_t e = hipSuccess;
   own = plan.ns_own > 0;
-  // (fp32 workgroups of one round need no order)
+  // (fp32: workgroups of one round, or of a few tiles, need no order, which takes a launch of 2 to 5 us)
   const long long own_wgs = (long long)shape->batch * shape->n_kv_heads * plan.ns_own * ((group + 15) / 16);
-  if (own && shape->batch > 1 && (shape->dtype == FB_BF16 ? plan.ns_shared == 0 : own_wgs > 256)) {
+  if (own && shape->batch > 1 && (shape->dtype == FB_BF16 ? plan.ns_shared == 0 : own_wgs > 256 && shape->prefix_len > 8 * fb::kKeyTile * plan.ns_own)) {
     if (shape->batch <= 128 && shape->dtype == FB_BF16) {
       p.order_inline = 1;
     } else {
