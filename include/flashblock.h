@@ -395,7 +395,8 @@ typedef struct fb_rows {
  * by `rotary`, v -> v_out moved, in one launch.  inverse = 0: from any rows (token-major: a token's q, k and v side by side) to any
  * rows, [B,H,Bq,d] the common case.  inverse = 1: by the opposite angles, which undoes it and, a rotation being orthogonal, is the
  * gradient: that of q_out in q, that of q's rows out.  Each of the pairs (q, q_out), (k, k_out), (v, v_out) may be NULL, but not
- * all three.  q has n_q_heads heads, k and v n_kv_heads; prefix_len and scale are ignored.  In place (equal data and strides) is allowed.
+ * all three.  q has n_q_heads heads, k and v n_kv_heads; prefix_len and scale are ignored.  An output may be its own input in place (equal
+ * data and strides); it overlaps no input else.
  */
 fb_status fb_rotate_block(const fb_shape* shape, const fb_rotary* rotary, int32_t inverse, const fb_rows* q, const fb_rows* k,
                           const fb_rows* v, const fb_rows* q_out, const fb_rows* k_out, const fb_rows* v_out, void* hip_stream);
@@ -404,7 +405,8 @@ fb_status fb_rotate_block(const fb_shape* shape, const fb_rotary* rotary, int32_
  * Block advance (Section 4.2: a finished block's keys and values join the prefix cache) on the paged cache, for a block, a prompt or
  * a single token of every sequence: rows i < append_lens[b] of k and v go to slots prefix_lens[b] + i of sequence b, whose
  * pages block_table lists; k is rotated on the way if `rotary` is given (NULL: written as it is).  The pools of kv are written;
- * prefix_lens is read only, and lens_out [batch] (may be NULL, may not be prefix_lens) gets the new lengths.
+ * prefix_lens is read only, and lens_out [batch] (may be NULL; FB_ERR_UNSUPPORTED where it overlaps prefix_lens, append_lens, block_table
+ * or the rotation's positions or first) gets the new lengths.
  *   append_lens  device, int32 [batch], clamped to [0, block_len]; NULL: block_len rows of every sequence.
  *   q, q_out     both or neither: all block_len rows of q, rotated at the same positions, go to q_out in the same launch
  *                (single-token decoding: what the attention after it takes).
@@ -421,13 +423,15 @@ fb_status fb_append_paged(const fb_shape* shape, const fb_paged_kv* kv, const fb
  * prefix_lens[b] keys by block_table as in fb_external_partial_paged.  The shared keys are read once for the rows of all sequences of a
  * KV head together, instead of once for every sequence.  Results are those of fb_external_partial_paged / fb_refresh_step_paged over the
  * keys in a row, up to the order of floating-point sums; one call has the same bits every time.
- *   kv            both kinds of pages are in its pools.  shape->prefix_len is the largest number of own keys; where it is 0, block_table,
- *                 prefix_lens and max_pages are not looked at.
+ *   kv            both kinds of pages are in its pools; page_size a multiple of 64.  shape->prefix_len is the largest number of own keys, at
+ *                 most 2^30; where it is 0, block_table, prefix_lens and max_pages are not looked at.
  *   shared_pages  device, int32 [ceil(shared_len / page_size)], each entry clamped into the pool; NULL iff shared_len is 0.  (Shared
  *                 keys in one dense slab [Hkv, P, d] are a pool of one page of P, a multiple of 64, keys.)
  *   shared_len    host, >= 0, at most 2^30.  A call captured into a graph keeps it.
  * Any of the two may be empty; with no key at all a row gets the empty partial.  workspace: >= fb_shared_workspace_bytes(shape, shared_len)
- * bytes, 0 on invalid arguments.  (Batches above 128 sequences add the sequence-ordering launch.)
+ * bytes, 0 on invalid arguments.  Launches of a step: bf16 two, the keys and what folds them with the block (blocks of more than 32 rows: three);
+ * fp32 three or four.  Own caches without shared keys, where they are long and of many sequences, and fp32 ones in several rounds of workgroups,
+ * take a sequence-ordering launch more.
  */
 size_t fb_shared_workspace_bytes(const fb_shape* shape, int32_t shared_len);
 fb_status fb_external_partial_shared(const fb_shape* shape, const void* q, const fb_paged_kv* kv, const int32_t* shared_pages,

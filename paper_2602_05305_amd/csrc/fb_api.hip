@@ -1177,10 +1177,19 @@ fb_status fb_append_paged(const fb_shape* shape, const fb_paged_kv* kv, const fb
   if (kv->num_pages <= 0 || kv->page_size <= 0 || kv->max_pages <= 0) return FB_ERR_SHAPE;
   if ((long long)kv->max_pages * kv->page_size < shape->prefix_len) return FB_ERR_SHAPE;
   if (!aligned16(kv->k_pool) || !aligned16(kv->v_pool)) return FB_ERR_ALIGN;
-  const uintptr_t out = reinterpret_cast<uintptr_t>(lens_out), lens = reinterpret_cast<uintptr_t>(kv->prefix_lens), bytes = 4 * (uintptr_t)shape->batch;
-  if (lens_out && out < lens + bytes && lens < out + bytes) return FB_ERR_UNSUPPORTED;      // other workgroups still read the lengths
-  if (((out | lens | reinterpret_cast<uintptr_t>(append_lens) | reinterpret_cast<uintptr_t>(kv->block_table)) & 3u) != 0) return FB_ERR_ALIGN;
-  if (rotary && (st = check_rotary(shape, rotary)) != FB_OK) return st;
+  // lens_out may be nothing that other workgroups still read
+  const auto meets = [&](const void* at, long long ints) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(at), out = reinterpret_cast<uintptr_t>(lens_out);
+    return at && lens_out && out < x + 4 * (uintptr_t)ints && x < out + 4 * (uintptr_t)shape->batch;
+  };
+  if (meets(kv->prefix_lens, shape->batch) || meets(append_lens, shape->batch) || meets(kv->block_table, (long long)shape->batch * kv->max_pages)) return FB_ERR_UNSUPPORTED;
+  if (((reinterpret_cast<uintptr_t>(lens_out) | reinterpret_cast<uintptr_t>(kv->prefix_lens) | reinterpret_cast<uintptr_t>(append_lens) | reinterpret_cast<uintptr_t>(kv->block_table)) & 3u) != 0)
+    return FB_ERR_ALIGN;
+  if (rotary) {
+    if ((st = check_rotary(shape, rotary)) != FB_OK) return st;
+    if (rotary->positions ? meets(rotary->positions, (shape->batch - 1) * rotary->position_stride + (long long)shape->block_len * rotary->n_axes) : meets(rotary->first, shape->batch))
+      return FB_ERR_UNSUPPORTED;
+  }
   if ((st = check_rows(shape, k, shape->n_kv_heads, false)) != FB_OK || (st = check_rows(shape, v, shape->n_kv_heads, false)) != FB_OK) return st;
   if (q && ((st = check_rows(shape, q, shape->n_q_heads, false)) != FB_OK || (st = check_rows(shape, q_out, shape->n_q_heads, true)) != FB_OK)) return st;
   fb::RotateParams p = rotate_params(shape, rotary, false);
@@ -1333,7 +1342,7 @@ fb_status shared_partials(const fb_shape* shape, const void* q, const fb_paged_k
   if (kv->struct_size != sizeof(fb_paged_kv)) return FB_ERR_SHAPE;
   bool own = shape->prefix_len > 0;
   if (shared_len < 0) return FB_ERR_SHAPE;
-  if (shared_len > (1 << 30)) return FB_ERR_UNSUPPORTED;
+  if (shared_len > (1 << 30) || shape->prefix_len > (1 << 30)) return FB_ERR_UNSUPPORTED;      // (keys are counted in 32 bits, a round of tiles beyond the last)
   if ((shared_len > 0 && !shared_pages) || (own && (!kv->block_table || !kv->prefix_lens))) return FB_ERR_NULL;
   if ((own || shared_len > 0) && (!kv->k_pool || !kv->v_pool)) return FB_ERR_NULL;
   if (kv->num_pages <= 0 || kv->page_size <= 0 || (own && kv->max_pages <= 0)) return FB_ERR_SHAPE;
@@ -1419,7 +1428,7 @@ fb_status shared_partials(const fb_shape* shape, const void* q, const fb_paged_k
 extern "C" {
 
 size_t fb_shared_workspace_bytes(const fb_shape* shape, int32_t shared_len) {
-  if (check_shape(shape) != FB_OK || shared_len < 0 || shared_len > (1 << 30)) return 0;
+  if (check_shape(shape) != FB_OK || shared_len < 0 || shared_len > (1 << 30) || shape->prefix_len > (1 << 30)) return 0;
   const SharedPlan plan = shared_plan(shape, shared_len);
   return std::max((size_t)256, ws_layout(shape, plan.ns_shared + plan.ns_own, 1, 0).total);
 }

@@ -203,3 +203,21 @@ def test_shared_workspace_query():
     assert fb.fb_shared_workspace_bytes(s, -1) == 0 and fb.fb_shared_workspace_bytes(_shape(batch=0), 64) == 0 and fb.fb_shared_workspace_bytes(s, (1 << 30) + 1) == 0
     n = fb.fb_shared_workspace_bytes(s, 1000)
     assert _shared(nbytes=n - 1) == fb.FB_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("kw", [
+    dict(counts=0x2000, lens_out=0x2000), dict(counts=0x2000, lens_out=0x2004), dict(counts=0x2004, lens_out=0x2000),
+    dict(kv=_paged(block_table=0x2000), lens_out=0x200c), dict(rotary=_rotary(first=0x2000), lens_out=0x2000),
+    dict(rotary=_rotary(positions=0x2000), lens_out=0x2008), dict(rotary=_rotary(positions=0x2000, position_stride=100), lens_out=0x2000 + 400 + 8),
+])
+def test_new_lengths_over_what_other_workgroups_read_are_refused(kw):
+    """batch 2, block_len 3, two pages a sequence"""
+    assert _append(**kw) == fb.FB_ERR_UNSUPPORTED
+
+
+def test_shared_counts_keys_in_32_bits():
+    long = _shape(prefix_len=(1 << 30) + 1)
+    kv = _paged(max_pages=1 << 25)
+    assert _shared(shape=long, kv=kv) == fb.FB_ERR_UNSUPPORTED
+    assert _shared(shape=long, kv=kv, step=(FAKE, FAKE, FAKE, None)) == fb.FB_ERR_UNSUPPORTED
+    assert fb.fb_shared_workspace_bytes(long, 64) == 0
