@@ -147,3 +147,46 @@ def test_an_infinite_value_of_the_last_shared_key(dtype, B, Hq, Hkv, d, Bq, shar
     assert np.isposinf(out[:, :first, :, 7]).all()
     out[:, :first, :, 7] = 0
     assert np.isfinite(out).all()
+
+
+# fp32: rows of the workgroups of the shared keys and of the own ones (64 with a wavefront's parts of the columns, or without: head_dim 64); of one kind
+# they are one launch; "order": sequences by length
+@pytest.mark.parametrize("B,Hq,Hkv,d,Bq,shared,own,page", [
+    (274, 1, 1, 64, 1, 70, 600, 64),          # 16 16 order
+    (137, 2, 2, 128, 1, 70, 600, 192),
+    (26, 8, 4, 64, 20, 70, 1, 64),            # 32 32
+    (13, 16, 2, 128, 20, 70, 65, 64),
+    (65, 2, 2, 64, 20, 130, 600, 64),         # 32 32 order
+    (132, 1, 1, 128, 20, 300, 600, 128),
+    (13, 32, 4, 64, 20, 70, 64, 64),          # 64 64
+    (26, 16, 2, 64, 20, 300, 200, 64),        # 64 in parts, both
+    (205, 2, 1, 128, 20, 70, 33, 64),
+    (131, 2, 1, 64, 20, 700, 600, 64),        # ... order
+    (133, 1, 1, 128, 40, 300, 600, 64),
+    (9, 1, 1, 64, 40, 70, 900, 64),           # 16 and 64
+    (13, 2, 1, 128, 20, 70, 600, 64),         # 16 and 64 in parts
+    (174, 8, 4, 64, 1, 300, 600, 64),         # 32 and 16, order
+    (171, 2, 2, 64, 4, 700, 600, 64),         # 64 and 16, order
+    (129, 2, 2, 128, 4, 1500, 600, 64),       # 64 in parts and 16, order
+    (87, 4, 4, 64, 1, 0, 600, 64),            # own keys alone, order
+])
+def test_routes_f32(B, Hq, Hkv, d, Bq, shared, own, page):
+    rng = np.random.default_rng(B * 1000 + own)
+    lens = rng.integers(0, own + 1, size=B)
+    lens[-1] = own
+    Case("f32", B, Hq, Hkv, d, Bq, shared, lens, page, seed=B).run()
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,d,Bq,shared", [(26, 8, 4, 64, 20, 70), (13, 16, 2, 128, 20, 70), (13, 32, 4, 64, 20, 70), (26, 16, 2, 64, 20, 300), (205, 2, 1, 128, 20, 70)])
+def test_infinite_values_of_last_keys_f32(B, Hq, Hkv, d, Bq, shared):
+    """The last shared key's in one column, one sequence's last own key's in another."""
+    c = Case("f32", B, Hq, Hkv, d, Bq, shared, [3] * B, 64)
+    c.v_pool[int(c.pages[(shared - 1) // 64]), 0, (shared - 1) % 64, 7] = float("inf")
+    c.v_pool[int(c.table[1, 0]), 0, 2, 9] = float("inf")
+    c.refresh()
+    torch.cuda.synchronize()
+    out = c.out.double().cpu().numpy()
+    first = Hq // Hkv
+    assert np.isposinf(out[:, :first, :, 7]).all() and np.isposinf(out[1, :first, :, 9]).all()
+    out[:, :first, :, 7] = out[1, :first, :, 9] = 0
+    assert np.isfinite(out).all()
