@@ -59,8 +59,8 @@ __device__ __forceinline__ void store_aligned(T* at, const Pack<T>& r) {
   *(Pack<T>*)__builtin_assume_aligned(at, 16) = r;
 }
 
-// Where the two packs of slot c start: pair j = V c + e has its members at first + e and second + e (halves), or the pack pair
-// holds pairs next to each other (adjacent, and what no pair covers).
+// A thread's two packs, pairs j0 .. j0 + V - 1.  Halves: the pairs' first members, from j0, and their second ones, from j0 + pairs.  Flat: the
+// elements 2 j0 .. 2 j0 + 2 V - 1 (adjacent members, or elements that no pair covers).  Mixed: each of its own, where the pairs end inside.
 enum SlotKind : int { kSlotHalves, kSlotFlat, kSlotMixed };
 
 // A workgroup: ROWS rows (token x head), a slot to a thread.  (More slots to a thread: 8 x 4096 tokens of 32 / 8 heads, head_dim 128, 1 / 2 / 4 / 8
