@@ -1221,9 +1221,9 @@ struct SharedPlan {
 // Where the own keys go: into the folding kernel, or as splits into the launch of the shared keys.  In us: a wavefront there takes 1.2 (head_dim
 // 64: 1.0) for each of its tiles, a quarter of the longest sequence's, a workgroup of the split pass 3 and 1.0 (0.7) for each of its; both
 // no less than half the largest length of every sequence takes at 4.5 TB/s.  Splits take the compute units that the rounds of the shared
-// keys leave, then rounds of their own, and are partials to fold.  (8400 random calls, own keys from 32 to 2048: the choice takes 0.6 % longer than
-// the best of both ways with 1 to 16 splits, 11 % in 99 of 100; always the folding kernel 5.9 and 57 %: 4 sequences of 8 rows and up to
-// 1905 keys 27.9 us there, 14.5 in 16 splits.)
+// keys leave, then rounds of their own, and are partials to fold.  (9500 random calls, own keys from 16 to 2048: the choice is level with the
+// best of both ways with 1 to 16 splits on average and takes 11 % longer in 99 of 100; always the folding kernel 6 and 70 %: 4 sequences of 8 rows
+// of 8 heads and up to 1905 keys 30.8 us there, 18.5 in 16 splits.)
 int own_splits(const fb_shape* s, const SharedPlan& plan, long long shared_wgs, double shared_us, double fold_us, int per_row) {
   const bool wide = s->head_dim == 128;
   const int tiles = (s->prefix_len + fb::kKeyTile - 1) / fb::kKeyTile;
@@ -1237,7 +1237,7 @@ int own_splits(const fb_shape* s, const SharedPlan& plan, long long shared_wgs, 
   int splits = 0;
   const long long shared_rounds = (shared_wgs + 255) / 256, free = shared_rounds * 256 - shared_wgs;
   const double pass = (double)shared_rounds * shared_us;
-  auto trips = [&](int n) { return 0.9 * (double)((plan.ns_shared + n + 4 * per_row - 1) / (4 * per_row)); };
+  auto trips = [&](int n) { return 0.3 * (double)((plan.ns_shared + n + 4 * per_row - 1) / (4 * per_row)); };
   for (int n = 1; n <= 16 && (n == 1 || n <= tiles); n *= 2) {
     const double wg = (double)((tiles + n - 1) / n) * (wide ? 1.0 : 0.7) + 3.0;
     const long long wgs = units * n, each = std::max(1ll, (long long)(shared_us / wg)), left = std::max(0ll, wgs - free * each);
@@ -1251,23 +1251,24 @@ int own_splits(const fb_shape* s, const SharedPlan& plan, long long shared_wgs, 
 }
 
 // Workgroups and splits of the shared keys' pass.  The least time by
-//   rounds of 256 workgroups * (tiles of a split * c + e), or the keys at 4.25 TB/s if that takes longer,
-//   + 0.145 us (head_dim 64: 0.108) for every MB of split partials, which are written and folded, + 0.9 us for every four of them that a
+//   rounds of 256 workgroups * (tiles of a split * c + e), or the keys at 5.2 TB/s if that takes longer,
+//   + 0.127 us (head_dim 64: 0.122) for every MB of split partials, which are written and folded, + 0.3 us for every four of them that a
 //   thread folds one after the other;
-// c and e in us by the rows of a workgroup.  Fitted to 41000 random calls (2 to 128 sequences, 256 to 32768 keys; off by 3 % at the median);
-// the choice takes 0.7 % longer than the best of all that were measured on average, 2.4 % in 90 and 9 % in 99 of 100.  Few rows: small
-// workgroups of long splits (4 sequences of 24 rows of 16 / 4 heads, 5003 keys, head_dim 64: 64 rows, 10 splits 17.7 us, 128 rows, 21 splits 18.7,
-// 256, 16 20.4); many rows: 256 (32 sequences of 8 rows of 4 / 4 heads, 10000 keys: 128 rows 39.2, 256 43.8; of 32 rows of 32 / 8, 32768 keys: 256 475).
+// c and e in us by the rows of a workgroup.  Fitted to 59000 random calls (2 to 128 sequences, 256 to 32768 keys; off by 3 % at the median);
+// the choice takes 1 % longer than the best of all that were measured on average, 4 % in 90 and 10 % in 99 of 100.  Few rows: small
+// workgroups (4 sequences of 24 rows of 16 / 4 heads, 5003 keys, head_dim 64: 64 rows, 10 splits 17.1 us, 128 rows, 21 splits 17.0,
+// 256, 16 19.1); many rows: 256 (32 sequences of 8 rows of 4 / 4 heads, 10000 keys: 128 rows, 32 splits 21.0, 256, 31 25.4; of 32 rows of 32 / 8, 32768
+// keys: 256 480).
 void plan_bf16(const fb_shape* s, int tiles, SharedPlan& plan) {
   static const struct { int rows; double c, e; } kinds[2][5] = {
-      {{32, 0.69, 1.6}, {64, 0.67, 1.8}, {128, 0.80, 2.2}, {256, 1.18, 1.9}, {256, 1.06, 3.2}},        // head_dim 64
-      {{32, 0.99, 1.9}, {64, 0.97, 2.2}, {128, 1.00, 2.6}, {256, 1.54, 2.6}, {256, 1.32, 5.4}}};       // 128
+      {{32, 0.70, 1.6}, {64, 0.68, 2.1}, {128, 0.82, 2.5}, {256, 1.25, 2.5}, {256, 1.04, 3.3}},        // head_dim 64
+      {{32, 1.01, 2.1}, {64, 0.99, 2.6}, {128, 1.03, 3.2}, {256, 1.56, 3.6}, {256, 1.32, 6.4}}};       // 128
   const bool wide = s->head_dim == 128;
   const long long nrows = rows_of(s) / s->n_kv_heads, group = (long long)(s->n_q_heads / s->n_kv_heads) * s->block_len;
-  const double keys = (double)tiles * fb::kKeyTile * s->n_kv_heads * s->head_dim * 4 / 4.25e6;
-  const double fold = (double)rows_of(s) * s->head_dim * 8e-6 * (wide ? 0.145 : 0.108);
+  const double keys = (double)tiles * fb::kKeyTile * s->n_kv_heads * s->head_dim * 4 / 5.2e6;
+  const double fold = (double)rows_of(s) * s->head_dim * 8e-6 * (wide ? 0.127 : 0.122);
   int per_row = 1;                                            // groups of threads that fold a row's splits
-  while (per_row < 32 && 32 / (2 * per_row) >= std::min(group, 32ll)) per_row *= 2;
+  while (per_row < 32 && 32 / (2 * per_row) >= std::min(group, (long long)fb::finish_rows((long long)s->batch * s->n_kv_heads, group))) per_row *= 2;
   double best = -1, wg_us = 0;
   long long wgs = 0;
   for (int k = 0; k < 5 && tiles > 0; ++k) {
@@ -1279,7 +1280,7 @@ void plan_bf16(const fb_shape* s, int tiles, SharedPlan& plan) {
       if (k == fb::kShared256 && tiles < 5 * ns) continue;
       const long long rounds = (groups * ns + 255) / 256;
       const double pass = std::max((double)rounds * ((double)((tiles + ns - 1) / ns) * kind.c + kind.e), keys);
-      const double cost = pass + fold * (double)ns + 0.9 * (double)((ns + 4 * per_row - 1) / (4 * per_row));
+      const double cost = pass + fold * (double)ns + 0.3 * (double)((ns + 4 * per_row - 1) / (4 * per_row));
       if (best < 0 || cost < best) {
         best = cost;
         plan.ns_shared = (int)ns;
@@ -1407,6 +1408,7 @@ fb_status shared_partials(const fb_shape* shape, const void* q, const fb_paged_k
     f->o = o_part; f->m = m_part; f->lse = lse_part;
     f->rows = (long long)rows;
     f->nsplit = ns;
+    f->wg_rows = fb::finish_rows((long long)shape->batch * shape->n_kv_heads, group);
     f->B = shape->batch; f->Hq = shape->n_q_heads; f->Hkv = shape->n_kv_heads; f->G = (int)G; f->Bq = shape->block_len;
     f->own_keys = plan.own_in_finish ? shape->prefix_len : 0;
     f->page_size = kv->page_size; f->max_pages = kv->max_pages; f->num_pages = kv->num_pages;

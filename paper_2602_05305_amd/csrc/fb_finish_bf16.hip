@@ -1,6 +1,6 @@
 // Second launch of a refresh step, or of an external pass, over a shared prefix (bf16, gfx950): folds the split partials of the first
-// launch (Eq. 5), streams a sequence's own pages, computes the block-internal attention (Eq. 7) and merges (Eq. 8-9), all for 32 rows of
-// one KV head of one sequence to a workgroup.
+// launch (Eq. 5), streams a sequence's own pages, computes the block-internal attention (Eq. 7) and merges (Eq. 8-9), all for up to 32 rows
+// of one KV head of one sequence to a workgroup (finish_rows: 32, or fewer where the workgroups would be few).
 //
 // What bounds it: HBM over the own keys where there are many; else the latency of a chain of four memory round trips (length, page, keys,
 // partials), which is why it is one kernel: passes of their own write the own partials and read them back, and each adds a launch.
@@ -107,11 +107,11 @@ __global__ __launch_bounds__(256, 2) void shared_finish_kernel(const FinishParam
   // ---- workgroup -> (row group, KV head, sequence)
   const uint32_t j8 = blockIdx.x >> 3, jq = fastdiv(j8, p.div_rowtiles), unit = jq * 8 + (blockIdx.x & 7);
   if (unit >= (uint32_t)(p.B * p.Hkv)) return;                // workgroup-uniform
-  const int row0 = (int)(j8 - jq * p.div_rowtiles.d) * 32;
+  const int row0 = (int)(j8 - jq * p.div_rowtiles.d) * p.wg_rows;
   int b = (int)fastdiv(unit, p.div_hkv);
   const int kvh = (int)(unit - (uint32_t)b * p.div_hkv.d);
   if (p.order != nullptr) b = sload(p.order, b);
-  const int valid = min(32, p.G * p.Bq - row0);
+  const int valid = min(p.wg_rows, p.G * p.Bq - row0);
   const size_t grow0 = (size_t)(b * p.Hq + kvh * p.G) * p.Bq + row0;
   // the first tile's page is asked for along with the length, used or not
   int nkeys = 0;
@@ -449,12 +449,12 @@ template <int D>
 hipError_t launch_finish(const FinishParams& p, hipStream_t s) {
   using C = NCfg<D>;
   FinishParams q = p;
-  const int rowtiles = (p.G * p.Bq + 31) / 32;
+  const int rowtiles = (p.G * p.Bq + p.wg_rows - 1) / p.wg_rows;
   q.div_rowtiles = make_fastdiv((uint32_t)rowtiles);
   q.div_hkv = make_fastdiv((uint32_t)p.Hkv);
   q.div_page = make_fastdiv((uint32_t)(p.page_size > 0 ? p.page_size : 1));
   const long long grid = ((long long)p.B * p.Hkv + 7) / 8 * 8 * rowtiles;
-  if (grid >= (1ll << 31) || (p.k_block != nullptr && (p.Bq > kFinishBlock || p.out == nullptr))) return hipErrorInvalidValue;
+  if (grid >= (1ll << 31) || p.wg_rows < 1 || p.wg_rows > 32 || (p.k_block != nullptr && (p.Bq > kFinishBlock || p.out == nullptr))) return hipErrorInvalidValue;
   static LdsLimit lim;
   hipError_t e = raise_lds_limit(shared_finish_kernel<D>, C::LDS, lim, C::LDS);
   if (e != hipSuccess) return e;

@@ -237,6 +237,14 @@ struct RotateParams {
 // largest number of them), and with k_block != null the block of at most kFinishBlock rows and the merge.
 constexpr int kFinishBlock = 32;
 constexpr int kFinishRound = 512;      // its workgroups on the chip at once
+// Rows of its workgroups, at most 32, for `heads` (sequence, KV head) pairs of `group` rows: fewer where all of them are one workgroup to a compute
+// unit at most, so that more threads fold a row's splits (us, 32 / 8 / 4 / 1 rows: 5 x 128 rows, 48 splits 47.9 / 36.8 / 36.3 / 42.6; 8 x 32 rows, 48 splits 31.2 / 20.3 /
+// 19.0 / 19.0; 64 x 16 rows, 12 splits, own keys to 512 27.6 / 25.9 / 26.3 / 32.1), and not beyond: own keys are read by each (140 x 136 rows 30.4 / 43.7 / 67.8 / 215).
+inline int finish_rows(long long heads, long long group) {
+  int rows = 32;
+  while (rows > 1 && heads * ((group + rows / 2 - 1) / (rows / 2)) <= 256) rows /= 2;
+  return rows;
+}
 struct FinishParams {
   const void* q; const void* k_pool; const void* v_pool; const void* k_block; const void* v_block;
   const int32_t* block_table; const int32_t* prefix_lens;
@@ -244,6 +252,7 @@ struct FinishParams {
   float* o; float* m; float* lse; void* out; float* lse_out;
   long long rows;              // of a split
   int nsplit, B, Hq, Hkv, G, Bq, own_keys, page_size, max_pages, num_pages;
+  int wg_rows;                 // of a workgroup
   const int32_t* order;        // sequences as workgroups take them, or null
   float scale_log2;
   FastDiv div_rowtiles, div_hkv, div_page;
