@@ -1240,10 +1240,8 @@ int own_splits(const fb_shape* s, const SharedPlan& plan, long long shared_wgs, 
   auto trips = [&](int n) { return 0.3 * (double)((plan.ns_shared + n + 4 * per_row - 1) / (4 * per_row)); };
   for (int n = 1; n <= 16 && (n == 1 || n <= tiles); n *= 2) {
     const double wg = (double)((tiles + n - 1) / n) * (wide ? 1.0 : 0.7) + 3.0;
-    const long long wgs = units * n, each = std::max(1ll, (long long)(shared_us / wg)), left = std::max(0ll, wgs - free * each);
-    double t = pass;
-    if (left > 0) t += (double)((left + 255) / 256) * wg;
-    else if (wgs > 0) t = std::max(pass, pass - shared_us + wg * (double)std::min(each, (wgs + free - 1) / std::max(free, 1ll)));
+    const long long left = std::max(0ll, units * n - free);
+    const double t = left > 0 ? pass + (double)((left + 255) / 256) * wg : std::max(pass, pass - shared_us + wg);
     const double cost = std::max({t - pass, keys - 0.5 * pass, 0.0}) + fold_us * n + trips(n) - trips(0) + (plan.ns_shared == 0 ? 4.0 : 0.0);
     if (cost < best) { best = cost; splits = n; }
   }

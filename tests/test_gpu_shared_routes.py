@@ -30,15 +30,19 @@ pytestmark = pytest.mark.gpu
     (9, 2, 2, 128, 11, 4199, 33, 64),
     (65, 16, 4, 64, 1, 8174, 1, 64),          # 256 of 8 wavefronts, finish
     (113, 32, 4, 128, 3, 2096, 1, 64),
-    (136, 2, 2, 128, 40, 1893, 70, 64),       # ... order, blocks the second launch leaves to the internal pass
-    (43, 8, 2, 128, 32, 2073, 1, 64),         # ... split
+    (43, 8, 2, 128, 32, 2073, 1, 64),
     (130, 8, 1, 64, 11, 970, 33, 64),
+    (136, 2, 2, 128, 40, 1893, 70, 64),       # ... order, blocks the second launch leaves to the internal pass
+    (27, 1, 1, 128, 200, 4179, 1500, 64),     # ... split
+    (4, 2, 2, 64, 200, 8095, 1500, 64),
     (130, 32, 4, 128, 3, 3239, 0, 64),        # 256 of 4, none
     (39, 8, 4, 64, 40, 2572, 1, 64),          # ... finish
     (134, 4, 4, 64, 8, 7741, 70, 128),        # ... order
     (97, 16, 4, 128, 8, 3113, 60, 64),        # ... finish
-    (45, 8, 4, 128, 31, 3962, 1, 256),        # ... split
+    (45, 8, 4, 128, 31, 3962, 1, 256),
     (103, 16, 2, 64, 8, 3588, 1, 64),
+    (4, 4, 2, 64, 200, 7168, 70, 64),         # ... split
+    (13, 4, 4, 128, 100, 7354, 3000, 64),
     (63, 2, 2, 128, 1, 75, 70, 64),           # one row to a workgroup of the second launch
     (2, 16, 4, 128, 8, 13937, 3, 128),
     (4, 8, 1, 128, 1, 4095, 99, 64),
