@@ -430,7 +430,7 @@ fb_status fb_append_paged(const fb_shape* shape, const fb_paged_kv* kv, const fb
  *   shared_len    host, >= 0, at most 2^30.  A call captured into a graph keeps it.
  * Any of the two may be empty; with no key at all a row gets the empty partial.  workspace: >= fb_shared_workspace_bytes(shape, shared_len)
  * bytes, 0 on invalid arguments.  Launches of a step: bf16 two, the keys and what folds them with the block (blocks of more than 32 rows: three);
- * fp32 three or four.  Own caches without shared keys, where they are long and of many sequences, and fp32 ones in several rounds of workgroups,
+ * fp32 two to four.  Own caches without shared keys, where they are long and of many sequences, and fp32 ones in several rounds of workgroups,
  * take a sequence-ordering launch more.
  */
 size_t fb_shared_workspace_bytes(const fb_shape* shape, int32_t shared_len);
