@@ -1385,9 +1385,12 @@ fb_status shared_partials(const fb_shape* shape, const void* q, const fb_paged_k
       if (e != hipSuccess) return hip_fail(e);
     }
   }
-  // the folding kernel's workgroups are more than one round: the longest sequences first (us, lengths spread to 1024 and 2048: batch 128, 16 rows a
-  // KV head 67.6 -> 59.7, batch 32, 128 rows 62.1 -> 54.5)
-  const bool by_length = plan.own_in_finish && plan.ns_shared > 0 && shape->batch > 1 && shape->batch * shape->n_kv_heads * ((group + 31) / 32) > fb::kFinishRound;
+  // the folding kernel's workgroups are a few rounds, and its longest ones long: the longest sequences first (us, lengths spread to the number of keys,
+  // head_dim 128: batch 128, 4 rows a KV head of 8, 256 / 512 / 1024 / 2048 keys 26.5 -> 26.9 / 37.4 -> 36.3 / 68.0 -> 62.3 / 117 -> 107; batch 32, 128 rows, 2048 keys 76 -> 65; head_dim
+  // 64, batch 128, 512 / 1024 24.1 -> 24.6 / 34.9 -> 33.7; but batch 512, 4096 workgroups 119 -> 133, batch 1024, 2048 of them 119 -> 125)
+  const long long finish_wgs = shape->batch * shape->n_kv_heads * ((group + 31) / 32);
+  const bool by_length = plan.own_in_finish && plan.ns_shared > 0 && shape->batch > 1 && shape->batch <= 256 && finish_wgs > fb::kFinishRound &&
+                         finish_wgs <= 4 * fb::kFinishRound && (long long)shape->prefix_len * shape->head_dim >= 65536;
   int32_t* order = by_length ? (int32_t*)(ws + w.order) : nullptr;
   if (shape->dtype == FB_BF16 && plan.ns_shared > 0) {
     e = fb::launch_shared_bf16(sh, p, order, plan.rows, shape->head_dim, stream);

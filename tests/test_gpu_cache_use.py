@@ -56,7 +56,8 @@ def test_heads_and_sequences_that_coincide(dtype):
 
 @pytest.mark.parametrize("dtype,B,Hq,Hkv,d,Bq,S,start,page,steps", [
     ("bf16", 5, 8, 2, 128, 1, 700, [0, 60, 63, 64, 126], 64, 5),
-    ("bf16", 140, 4, 4, 128, 4, 70, [i % 60 for i in range(140)], 64, 3),        # sequences by length
+    ("bf16", 140, 4, 4, 128, 4, 70, [i % 60 for i in range(140)], 64, 3),
+    ("bf16", 140, 4, 4, 128, 1, 70, [(37 * i) % 561 for i in range(140)], 64, 3),      # sequences by length
     ("bf16", 22, 1, 1, 128, 1, 10, [6 * i for i in range(22)], 64, 4),           # own keys as splits
     ("bf16", 3, 4, 2, 64, 40, 300, [0, 30, 100], 128, 3),
     ("bf16", 4, 4, 2, 64, 2, 0, [0, 5, 62, 200], 64, 3),                         # nothing shared

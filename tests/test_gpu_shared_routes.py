@@ -12,32 +12,38 @@ from test_gpu_shared import Case
 pytestmark = pytest.mark.gpu
 
 
-# rows of the first launch's workgroups (256: of 8 wavefronts, or of 4); own keys: "finish", "order" (more than one round), "split", "none"
+# rows of the first launch's workgroups (256: of 8 wavefronts, or of 4); own keys: "finish", "order" (long ones, several rounds: sequences by length), "split", "none"
 @pytest.mark.parametrize("B,Hq,Hkv,d,Bq,shared,own,page", [
     (108, 4, 4, 64, 1, 65, 1, 64),            # 32 rows, finish
     (50, 8, 4, 64, 1, 2087, 1, 192),
     (131, 2, 2, 64, 1, 5460, 70, 64),
-    (133, 4, 4, 64, 1, 62, 30, 64),           # 32, order
+    (133, 4, 4, 64, 1, 62, 30, 64),           # ... in two rounds
     (139, 4, 4, 128, 4, 70, 33, 128),
+    (133, 4, 4, 64, 1, 62, 1100, 64),         # 32, order
+    (139, 4, 4, 128, 4, 70, 600, 128),
     (22, 1, 1, 128, 1, 10, 140, 64),          # 32, split
     (33, 1, 1, 128, 4, 6777, 300, 64),        # 32, finish
-    (138, 4, 4, 64, 16, 25, 65, 64),          # 64, order
+    (138, 4, 4, 64, 16, 25, 65, 64),          # 64, finish
+    (138, 4, 4, 64, 16, 25, 1050, 64),        # 64, order
     (35, 2, 2, 128, 1, 4144, 70, 64),         # 64, split
     (33, 8, 4, 128, 2, 1543, 33, 64),         # 128, finish
     (11, 8, 4, 64, 3, 6221, 1, 64),
-    (132, 4, 4, 128, 1, 1590, 100, 64),       # 128, order
+    (132, 4, 4, 128, 1, 1590, 100, 64),
+    (132, 4, 4, 128, 1, 1590, 520, 64),       # 128, order
     (65, 2, 1, 64, 32, 982, 1, 64),           # 128, split
     (9, 2, 2, 128, 11, 4199, 33, 64),
     (65, 16, 4, 64, 1, 8174, 1, 64),          # 256 of 8 wavefronts, finish
     (113, 32, 4, 128, 3, 2096, 1, 64),
     (43, 8, 2, 128, 32, 2073, 1, 64),
     (130, 8, 1, 64, 11, 970, 33, 64),
-    (136, 2, 2, 128, 40, 1893, 70, 64),       # ... order, blocks the second launch leaves to the internal pass
+    (136, 2, 2, 128, 40, 1893, 70, 64),       # ... blocks that the second launch leaves to the internal pass
+    (136, 2, 2, 128, 40, 1893, 530, 64),      # ... order
     (27, 1, 1, 128, 200, 4179, 1500, 64),     # ... split
     (4, 2, 2, 64, 200, 8095, 1500, 64),
     (130, 32, 4, 128, 3, 3239, 0, 64),        # 256 of 4, none
     (39, 8, 4, 64, 40, 2572, 1, 64),          # ... finish
-    (134, 4, 4, 64, 8, 7741, 70, 128),        # ... order
+    (134, 4, 4, 64, 8, 7741, 70, 128),
+    (134, 4, 4, 64, 8, 7741, 1030, 128),      # ... order
     (97, 16, 4, 128, 8, 3113, 60, 64),        # ... finish
     (45, 8, 4, 128, 31, 3962, 1, 256),
     (103, 16, 2, 64, 8, 3588, 1, 64),
